@@ -279,6 +279,73 @@ int dppo_loss_fwd_bwd(const dppo_head_shape* shape, const dppo_loss_params* p, i
                       void* dH, float* dW,
                       void* ws, size_t ws_bytes, void* stream);
 
+/* --------------------------------------------------------------------------------
+ * Token statistics of the LM head, next to dppo_token_logprob: for every loss token the entropy of the
+ * whole distribution and its most likely alternatives beside log-probability and lse, their gradients, and
+ * the same head in 8-bit integers.
+ *
+ * Arguments as in the section above, with these additions.
+ *   dtype 2 (dppo_token_stats only): H and W are int8 rows of D bytes, D a multiple of 128 and at most 131072
+ *     (dppo_quantize_rows pads rows with zeros); h_scale[T] and w_scale[V] are their scales, NULL for the other types.
+ *     z[n, v] = (float)(exact integer sum) * w_scale[v] * h_scale[row], rounded to float32 after each step.
+ *   ids may be NULL where no target is needed (no logp, no g_logp): a loss_pos entry is then valid in all of [0, T).
+ *
+ * With p = softmax(z[n, :]):
+ *   lse[n] = log sum_v exp z[n,v],  logp[n] = z[n,y_n] - lse[n],  entropy[n] = -sum_v p log p  (each may be NULL),
+ *   top_ids[n*top_k + i], top_logp[...] = id and log-probability of the i-th largest logit, equal logits in the
+ *   order of their ids; 0 <= top_k <= min(DPPO_TOP_K_MAX, V), both NULL for 0.
+ * Sums are float32 (against the maximum, so that neither lse nor entropy loses digits to large logits); logits at
+ * -infinity carry no weight. A row with a NaN logit or one at +infinity has NaN results; its top_ids are still distinct
+ * and in [0, V). V is at most 2^30. ws must be 256-byte aligned; a smaller workspace than recommended means
+ * smaller token chunks and does not change what a token's results are, except for their last bits.
+ */
+#define DPPO_TOP_K_MAX 64
+
+/* Recommended and smallest workspace (0 if the arguments are invalid). want_backward: 0 = dppo_token_stats,
+ * 1 = dppo_token_stats_bwd with a float32 dW, 2 = with a bfloat16 dW (top_k is not used by 1 and 2). */
+size_t dppo_token_stats_workspace_bytes(const dppo_head_shape* shape, int32_t top_k, int want_backward);
+size_t dppo_token_stats_workspace_min_bytes(const dppo_head_shape* shape, int32_t top_k, int want_backward);
+
+int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k,
+                     const void* H, const void* W, const float* h_scale /* int8 only */, const float* w_scale /* int8 only */,
+                     const int32_t* ids /* or NULL */, const int32_t* loss_pos /* or NULL */,
+                     float* logp /* or NULL */, float* lse /* or NULL */, float* entropy /* or NULL */,
+                     int32_t* top_ids, float* top_logp, int32_t* status /* or NULL */,
+                     void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of a loss through logp, lse and entropy, given dL/dlogp, dL/dlse and dL/dentropy per loss token (each may be NULL
+ * = 0, but not all three) and the lse and entropy (needed with g_entropy) that dppo_token_stats returned for the same H and W:
+ *   dz[n,v] = g_logp (1[v = y_n] - p) + g_lse p - g_entropy p (log p + entropy),
+ *   dH[T,D] = dz W (dtype of H; rows that are no loss rows are zero),  dW[V,D] = dz^T H.
+ * dW_dtype 0: float32, added to the buffer's contents if accumulate_dW != 0. dW_dtype 1: bfloat16 (bfloat16 operands only),
+ * overwritten: the float32 sum over all tokens, rounded once. dW is used for partial sums of dH before it is written.
+ * bfloat16 operands: dz is rounded to bfloat16 as an operand of the two products. dtype 2 has no gradient. */
+typedef struct {
+    int32_t accumulate_dW;
+    int32_t dW_dtype;      /* 0 = float32, 1 = bfloat16 */
+} dppo_stats_grad_params;
+
+int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_params* p,
+                         const void* H, const void* W, const int32_t* ids /* or NULL */, const int32_t* loss_pos /* or NULL */,
+                         const float* lse, const float* entropy /* or NULL */,
+                         const float* g_logp /* or NULL */, const float* g_lse /* or NULL */, const float* g_entropy /* or NULL */,
+                         void* dH, void* dW, int32_t* status /* or NULL */,
+                         void* ws, size_t ws_bytes, void* stream);
+
+/* dppo_quantize_rows -- X[rows, D] (dtype 0 float32, 1 bfloat16, contiguous) to 8 bits with one scale per row, tokens and
+ * vocabulary rows alike: scale[r] = max|X[r]| * (1/127), the reciprocal in float32, q[r, d] = X[r, d] / scale[r] (a correctly
+ * rounded float32 division) rounded to the nearest integer, ties to even, in [-127, 127]. A zero row has scale 0 and q 0; a row
+ * that holds an infinity or NaN has scale NaN and q 0. q has a row pitch of q_pitch bytes, a multiple of 128 of at least D; the
+ * columns behind D are set to 0. */
+int dppo_quantize_rows(int64_t rows, int32_t D, int32_t dtype, const void* X,
+                       int8_t* q, int64_t q_pitch, float* scale, void* stream);
+
+/* dppo_matmul_i8 -- Y[T, V] = X W^T of int8 rows with their scales (as dtype 2 above): the logits of a quantised head for a
+ * sampler, or any linear layer. Integer sums are exact; out_dtype 0: float32, 1: bfloat16 (rounded once from the float32 value).
+ * X[T, D] and W[V, D] 16-byte aligned, D a multiple of 128 of at most 131072; Y row-major with pitch V. */
+int dppo_matmul_i8(int64_t T, int32_t V, int32_t D, const int8_t* X, const float* x_scale,
+                   const int8_t* W, const float* w_scale, void* Y, int32_t out_dtype, void* stream);
+
 /* dppo_variance_terms -- App. D (variance of the rescaled single-sample estimator
  * gamma(q) gamma(o,q) g(q,o), q and o drawn from the pruned densities) for one scalar component
  * g[Q*G] of the gradient term and the prune probabilities reported by dppo_select.

@@ -21,7 +21,9 @@ _lib = None
 EXPORTS = ["dppo_status_str", "dppo_last_error", "dppo_select", "dppo_pack", "dppo_gather_f32", "dppo_token_norm_coef", "dppo_variance_terms",
            "dppo_workspace_bytes", "dppo_workspace_min_bytes", "dppo_token_logprob", "dppo_loss_fwd_bwd",
            "dppo_timing_enable", "dppo_timing_read", "dppo_history_update", "dppo_token_logprob_noalloc",
-           "dppo_static_scratch_bytes", "dppo_mfma_rate_probe", "dppo_timing_tile_phases"]
+           "dppo_static_scratch_bytes", "dppo_mfma_rate_probe", "dppo_timing_tile_phases",
+           "dppo_token_stats", "dppo_token_stats_bwd", "dppo_token_stats_workspace_bytes",
+           "dppo_token_stats_workspace_min_bytes", "dppo_quantize_rows", "dppo_matmul_i8"]
 STAGES = ["logits_gemm", "grad_logits", "dh_gemm", "dw_gemm", "elementwise"]
 
 
@@ -52,6 +54,10 @@ class LossParams(ctypes.Structure):
     _fields_ = [("clip_lo", c_float), ("clip_hi", c_float), ("beta", c_float),
                 ("accumulate_dW", c_int32), ("recompute_logits", c_int32),
                 ("ratio_level", c_int32), ("aggregation", c_int32), ("max_seq_tokens", c_int32)]
+
+
+class StatsGradParams(ctypes.Structure):
+    _fields_ = [("accumulate_dW", c_int32), ("dW_dtype", c_int32)]
 
 
 HEAD_BAD_TARGET, HEAD_BAD_POSITION, HEAD_SEQ_TOO_LONG = 1, 2, 4     # bits of the LM-head calls' device status word
@@ -109,6 +115,19 @@ def load():
     lib.dppo_timing_enable.argtypes = [c_int]
     lib.dppo_timing_read.restype = c_int
     lib.dppo_timing_read.argtypes = [POINTER(ctypes.c_double), POINTER(c_int64), c_int]
+    lib.dppo_token_stats_workspace_bytes.restype = c_size_t
+    lib.dppo_token_stats_workspace_bytes.argtypes = [POINTER(HeadShape), c_int32, c_int]
+    lib.dppo_token_stats_workspace_min_bytes.restype = c_size_t
+    lib.dppo_token_stats_workspace_min_bytes.argtypes = [POINTER(HeadShape), c_int32, c_int]
+    lib.dppo_token_stats.restype = c_int
+    lib.dppo_token_stats.argtypes = [POINTER(HeadShape), c_int32] + [c_void_p] * 13 + [c_size_t, c_void_p]
+    lib.dppo_token_stats_bwd.restype = c_int
+    lib.dppo_token_stats_bwd.argtypes = ([POINTER(HeadShape), POINTER(StatsGradParams)] + [c_void_p] * 13
+                                         + [c_size_t, c_void_p])
+    lib.dppo_quantize_rows.restype = c_int
+    lib.dppo_quantize_rows.argtypes = [c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int64, c_void_p, c_void_p]
+    lib.dppo_matmul_i8.restype = c_int
+    lib.dppo_matmul_i8.argtypes = [c_int64, c_int32, c_int32] + [c_void_p] * 5 + [c_int32, c_void_p]
     _lib = lib
     return lib
 
@@ -384,6 +403,178 @@ def dppo_loss_fwd_bwd(H, W, ids, loss_pos, loss_cu, seq_adv, seq_coef, logp_old,
     res["dH"] = dH
     res["dW"] = dW
     return res
+
+
+# --------------------------------------------------------------------------------------
+TOP_K_MAX = 64
+I8_ROW = 128       # rows of int8 operands are padded with zeros to a multiple of this many bytes
+_STATS_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int8: 2}
+
+
+def _arg(t, name: str, dtype, shape: tuple, device):
+    """A checked tensor argument (None passes): the library reads and writes what these say and no more."""
+    if t is None:
+        return None
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s (got %s %s on %s)"
+                         % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
+    return t
+
+
+class _on_device:
+    """Makes a tensor's device the current one for a call (the library launches on the current device)."""
+
+    def __init__(self, device):
+        if device.type != "cuda":
+            raise ValueError("the DPPO library takes device tensors only")
+        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _stats_shape(H, W, ids, loss_pos, status) -> HeadShape:
+    if H.dtype not in _STATS_DTYPES or H.dim() != 2 or W.dim() != 2:
+        raise ValueError("H [T,D] and W [V,D] must be float32, bfloat16 or int8 matrices")
+    T, D = H.shape
+    _arg(H, "H", H.dtype, (T, D), H.device)
+    _arg(W, "W", H.dtype, (W.shape[0], D), H.device)
+    _arg(ids, "ids", torch.int32, (T,), H.device)
+    if loss_pos is not None:
+        _arg(loss_pos, "loss_pos", torch.int32, (loss_pos.numel(),), H.device)
+    _arg(status, "status", torch.int32, (1,), H.device)
+    return HeadShape(T, T if loss_pos is None else loss_pos.numel(), D, W.shape[0], _STATS_DTYPES[H.dtype])
+
+
+def _stats_workspace(ws, shape, top_k, what, device) -> torch.Tensor:
+    if ws is None:
+        return alloc_workspace(load().dppo_token_stats_workspace_bytes(ctypes.byref(shape), top_k, what), device)
+    return _arg(ws, "ws", torch.uint8, (ws.numel(),), device)
+
+
+def dppo_token_stats_workspace_bytes(T: int, N: int, D: int, V: int, dtype_code: int, top_k: int = 0,
+                                     want_backward: int = 0) -> int:
+    """want_backward: 0 = dppo_token_stats, 1 = dppo_token_stats_bwd with a float32 dW, 2 = with a bfloat16 dW."""
+    shape = HeadShape(T, N, D, V, dtype_code)
+    return int(load().dppo_token_stats_workspace_bytes(ctypes.byref(shape), top_k, want_backward))
+
+
+def dppo_token_stats_workspace_min_bytes(T: int, N: int, D: int, V: int, dtype_code: int, top_k: int = 0,
+                                         want_backward: int = 0) -> int:
+    shape = HeadShape(T, N, D, V, dtype_code)
+    return int(load().dppo_token_stats_workspace_min_bytes(ctypes.byref(shape), top_k, want_backward))
+
+
+def dppo_token_stats(H, W, ids=None, loss_pos=None, top_k: int = 0, h_scale=None, w_scale=None,
+                     ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> dict:
+    """H [T,D], W [V,D] float32, bfloat16, or int8 with h_scale [T] and w_scale [V] (dppo_quantize_rows); ids [T] int32
+    or None (no logp). Returns dict(logp[N] or None, lse[N], entropy[N], top_ids[N,top_k] and top_logp[N,top_k], None for
+    top_k = 0) of device tensors; status: see dppo_token_logprob."""
+    lib = load()
+    device = H.device
+    shape = _stats_shape(H, W, ids, loss_pos, status)
+    N = shape.N
+    _arg(h_scale, "h_scale", torch.float32, (shape.T,), device)
+    _arg(w_scale, "w_scale", torch.float32, (shape.V,), device)
+    with _on_device(device):
+        ws = _stats_workspace(ws, shape, top_k, 0, device)
+        rooms = [N + 3 & -4] * 3
+        lse, entropy, logp = _pieces(torch.empty(sum(rooms), dtype=torch.float32, device=device), [N] * 3, rooms)
+        if ids is None:
+            logp = None
+        top_ids = top_logp = None
+        if top_k > 0:
+            top_ids = torch.empty((N, top_k), dtype=torch.int32, device=device)
+            top_logp = torch.empty((N, top_k), dtype=torch.float32, device=device)
+        st = lib.dppo_token_stats(ctypes.byref(shape), top_k, _ptr(H), _ptr(W), _ptr(h_scale), _ptr(w_scale), _ptr(ids),
+                                  _ptr(loss_pos), _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(top_ids), _ptr(top_logp),
+                                  _ptr(status), _ptr(ws), ws.numel(), _stream(device))
+        _check(st, "dppo_token_stats")
+    return dict(logp=logp, lse=lse, entropy=entropy, top_ids=top_ids, top_logp=top_logp)
+
+
+def dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy=None, g_logp=None, g_lse=None, g_entropy=None,
+                         dH: Optional[torch.Tensor] = None, dW: Optional[torch.Tensor] = None, accumulate_dW: bool = False,
+                         dW_dtype: torch.dtype = torch.float32, ws: Optional[torch.Tensor] = None,
+                         status: Optional[torch.Tensor] = None) -> dict:
+    """Gradients of a loss given its derivatives by logp, lse and entropy ([N] float32 each or None), with lse and entropy as
+    dppo_token_stats returned them. Returns dict(dH[T,D], dW[V,D] of dW_dtype or of the buffer handed in)."""
+    lib = load()
+    device = H.device
+    shape = _stats_shape(H, W, ids, loss_pos, status)
+    if H.dtype == torch.int8:
+        raise ValueError("H and W must be float32 or bfloat16")
+    for name, t in dict(lse=lse, entropy=entropy, g_logp=g_logp, g_lse=g_lse, g_entropy=g_entropy).items():
+        _arg(t, name, torch.float32, (shape.N,), device)
+    if dW is None:
+        if accumulate_dW:
+            raise ValueError("accumulate_dW needs the dW buffer to accumulate into")
+    else:
+        dW_dtype = dW.dtype
+        _arg(dW, "dW", dW_dtype, tuple(W.shape), device)
+    if dW_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("dW must be float32 or bfloat16")
+    _arg(dH, "dH", H.dtype, tuple(H.shape), device)
+    with _on_device(device):
+        ws = _stats_workspace(ws, shape, 0, 2 if dW_dtype == torch.bfloat16 else 1, device)
+        if dH is None:
+            dH = torch.empty_like(H)
+        if dW is None:
+            dW = torch.empty(W.shape, dtype=dW_dtype, device=device)
+        p = StatsGradParams(1 if accumulate_dW else 0, _STATS_DTYPES[dW_dtype])
+        st = lib.dppo_token_stats_bwd(ctypes.byref(shape), ctypes.byref(p), _ptr(H), _ptr(W), _ptr(ids), _ptr(loss_pos),
+                                      _ptr(lse), _ptr(entropy), _ptr(g_logp), _ptr(g_lse), _ptr(g_entropy), _ptr(dH), _ptr(dW),
+                                      _ptr(status), _ptr(ws), ws.numel(), _stream(device))
+        _check(st, "dppo_token_stats_bwd")
+    return dict(dH=dH, dW=dW)
+
+
+def dppo_quantize_rows(X: torch.Tensor):
+    """X [rows, D] float32 or bfloat16 -> (q [rows, D rounded up to a multiple of 128] int8, padded with zeros,
+    scale [rows] float32) with X ~ q[:, :D] * scale[:, None]."""
+    lib = load()
+    if X.dtype not in (torch.float32, torch.bfloat16) or X.dim() != 2:
+        raise ValueError("X must be a float32 or bfloat16 matrix")
+    rows, D = X.shape
+    device = X.device
+    _arg(X, "X", X.dtype, (rows, D), device)
+    pitch = (D + I8_ROW - 1) // I8_ROW * I8_ROW
+    with _on_device(device):
+        q = torch.empty((rows, pitch), dtype=torch.int8, device=device)
+        scale = torch.empty(rows, dtype=torch.float32, device=device)
+        _check(lib.dppo_quantize_rows(rows, D, _STATS_DTYPES[X.dtype], _ptr(X), _ptr(q), pitch, _ptr(scale), _stream(device)),
+               "dppo_quantize_rows")
+    return q, scale
+
+
+def dppo_matmul_i8(X, x_scale, W, w_scale, out_dtype: torch.dtype = torch.float32,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """X [T,D] int8 with x_scale [T], W [V,D] int8 with w_scale [V] -> Y [T,V] = X W^T * w_scale * x_scale, float32 or bfloat16."""
+    lib = load()
+    device = X.device
+    if X.dim() != 2 or W.dim() != 2:
+        raise ValueError("X [T,D] and W [V,D] must be int8 matrices")
+    (T, D), V = X.shape, W.shape[0]
+    _arg(X, "X", torch.int8, (T, D), device)
+    _arg(W, "W", torch.int8, (V, D), device)
+    _arg(x_scale, "x_scale", torch.float32, (T,), device)
+    _arg(w_scale, "w_scale", torch.float32, (V,), device)
+    if out is not None:
+        out_dtype = out.dtype
+        _arg(out, "out", out_dtype, (T, V), device)
+    if out_dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("the result is float32 or bfloat16")
+    with _on_device(device):
+        if out is None:
+            out = torch.empty((T, V), dtype=out_dtype, device=device)
+        _check(lib.dppo_matmul_i8(T, V, D, _ptr(X), _ptr(x_scale), _ptr(W), _ptr(w_scale), _ptr(out), _STATS_DTYPES[out_dtype],
+                                  _stream(device)), "dppo_matmul_i8")
+    return out
 
 
 def dppo_mfma_rate_probe(random_operands: bool, iters: int, out: torch.Tensor) -> float:

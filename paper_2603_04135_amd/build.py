@@ -13,7 +13,8 @@ INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 LIB_PATH = os.path.join(PKG_DIR, "libdppo_hip.so")
 
-SOURCES = ["api.hip", "select.hip", "pack.hip", "head_kernels.hip", "gemm_f32.hip", "gemm_mfma.hip"]
+SOURCES = ["api.hip", "select.hip", "pack.hip", "head_kernels.hip", "gemm_f32.hip", "gemm_mfma.hip",
+           "stats_api.hip", "stats_rows.hip", "quantize.hip", "gemm_stats.hip", "gemm_i8.hip"]
 COMMON_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

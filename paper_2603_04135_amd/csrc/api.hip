@@ -7,7 +7,7 @@
 #include <mutex>
 #include <vector>
 
-#include "dppo_internal.h"
+#include "api_internal.h"
 #include "gemm_f32_plan.h"
 
 namespace dppo {
@@ -47,23 +47,23 @@ struct TimingState {
 };
 TimingState g_timing;
 
-struct StageTimer {
-    int stage; hipStream_t st; hipEvent_t a = nullptr, b = nullptr;
-    StageTimer(int stage_, hipStream_t st_) : stage(stage_), st(st_) {
-        std::lock_guard<std::mutex> lk(g_timing.mu);
-        if (!g_timing.on || g_timing.spans.size() >= (1u << 16)) return;
-        a = g_timing.get(); b = g_timing.get();
-        if (a && b) (void)hipEventRecord(a, st); else a = b = nullptr;
-    }
-    ~StageTimer() {
-        if (!a) return;
-        (void)hipEventRecord(b, st);
-        std::lock_guard<std::mutex> lk(g_timing.mu);
-        g_timing.spans.push_back({stage, a, b});
-    }
-};
+}  // namespace
 
-constexpr int32_t CHUNK_ALIGN = 256;      // token-chunk granularity (= GEMM tile edge)
+StageTimer::StageTimer(int stage_, hipStream_t st_) : stage(stage_), st(st_) {
+    std::lock_guard<std::mutex> lk(g_timing.mu);
+    if (!g_timing.on || g_timing.spans.size() >= (1u << 16)) return;
+    a = g_timing.get(); b = g_timing.get();
+    if (a && b) (void)hipEventRecord(a, st); else a = b = nullptr;
+}
+StageTimer::~StageTimer() {
+    if (!a) return;
+    (void)hipEventRecord(b, st);
+    std::lock_guard<std::mutex> lk(g_timing.mu);
+    g_timing.spans.push_back({stage, a, b});
+}
+
+namespace {
+
 constexpr int32_t CHUNK_MAX = 32768;      // largest token chunk
 // The chunk's gathered hidden states [n_cp, D] are the operand that every tile row of the vocabulary GEMM
 // (and, transposed, of the dW GEMM) reads again; they must stay resident in the 256 MB Infinity Cache next
@@ -73,7 +73,9 @@ int32_t chunk_max_for(int32_t D, size_t es) {
     const int64_t fit = (int64_t)(CHUNK_CACHE_BYTES / ((size_t)D * es)) / CHUNK_ALIGN * CHUNK_ALIGN;
     return (int32_t)(fit < CHUNK_ALIGN ? CHUNK_ALIGN : (fit > CHUNK_MAX ? CHUNK_MAX : fit));
 }
-constexpr size_t REGION_ALIGN = 256;
+
+}  // namespace
+
 // Up to 4096 + D loss tokens the dH GEMM reads W as it lies, [K, N], instead of a transposed blocked copy of it: the GEMM
 // takes longer, by a share that falls with D, and the copy costs two passes over W. The line lies below every crossing
 // measured. Whole call, copy / W as it lies: D = 512, V = 151936 4000 tokens 1.861 / 1.825 ms, 5000 2.283 / 2.287; D = 1024,
@@ -81,6 +83,8 @@ constexpr size_t REGION_ALIGN = 256;
 // 3.364; D = 2560, V = 151936 6000 tokens 10.69 / 10.64, 7000 12.31 / 12.33; D = 4096, V = 151936 2000 tokens 6.58 / 6.11,
 // 8000 21.77 / 21.61, 12000 32.23 / 32.22.
 bool reads_w_directly(int64_t N, int32_t D) { return N <= 4096 + (int64_t)D; }
+
+namespace {
 
 struct WsPlan {
     int32_t Vp, n_tiles, n_cp;     // padded vocabulary, row tiles of the vocabulary GEMM, chunk rows
@@ -96,8 +100,6 @@ struct WsPlan {
     int f32_parts;                 // float32: sums of all rows of a chunk that the scratch of a dH GEMM cut along K holds
     size_t total;
 };
-
-int32_t round_up32(int64_t x, int32_t a) { return (int32_t)((x + a - 1) / a * a); }
 
 // Lays the workspace out for chunk size n_cp (multiple of CHUNK_ALIGN): the per-call regions, then `sets`
 // copies of the per-chunk regions (the offsets are those of set 0; set i lies i * chunk_bytes further on).
@@ -148,6 +150,10 @@ void layout(const dppo_head_shape& s, bool bwd, int32_t n_cp, WsPlan& p, int set
     p.total = p.fixed_bytes + (size_t)sets * p.chunk_bytes;
 }
 
+constexpr double CHUNK_OVERHEAD_ROUNDS = 0.35;
+
+}  // namespace
+
 // Chunk size for N loss tokens: balanced chunks of at most CHUNK_MAX tokens, their number chosen so
 // that the dH GEMM (tiles of 256 tokens x 256 columns, one workgroup per compute unit, so it runs in
 // rounds of one tile per compute unit) wastes little of its last round. Cost of a chunk in dH rounds: whole
@@ -157,8 +163,6 @@ void layout(const dppo_head_shape& s, bool bwd, int32_t n_cp, WsPlan& p, int set
 // its size (the dW read-modify-write, the small kernels, ramps). A chunk that overwrites dW may also cut a fuller last round, with
 // its parts in dW's memory; that is not priced. It is the first chunk only, and never the call's choice where one chunk holds all
 // tokens: a round more than half full, priced as whole, still costs less than the same tiles in two chunks or more.
-constexpr int DEFAULT_CUS = 256;          // MI355X; used where no device is at hand (size queries)
-constexpr double CHUNK_OVERHEAD_ROUNDS = 0.35;
 int32_t target_chunk(int64_t N, int32_t D, int32_t V, size_t es, int cus) {
     if (N <= 0) return CHUNK_ALIGN;
     const int64_t CHIP_CUS = cus > 0 ? cus : DEFAULT_CUS;
@@ -179,6 +183,8 @@ int32_t target_chunk(int64_t N, int32_t D, int32_t V, size_t es, int cus) {
     }
     return round_up32(ceil_div(N, best_c), CHUNK_ALIGN);
 }
+
+namespace {
 
 int validate_shape(const dppo_head_shape* s) {
     if (!s) return fail(DPPO_ERR_INVALID_ARG, "shape is NULL");
@@ -221,8 +227,6 @@ int plan_for(const dppo_head_shape& s, bool bwd, size_t ws_bytes, int cus, WsPla
     p.n_chunks = s.N > 0 ? ceil_div(s.N, p.n_cp) : 0;
     return DPPO_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Forward statistics of one chunk: Hc, targets, log-probs, lse. `ws` is the base of the set of
 // per-chunk regions to use (the workspace itself for set 0); no per-call region is touched. With keep_z the chunk's logits

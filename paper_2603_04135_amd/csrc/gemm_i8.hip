@@ -1,0 +1,26 @@
+// 8-bit integer GEMMs: C[n, V] = (int8 H) (int8 W)^T with exact int32 sums, a scale per token and one per vocabulary row.
+#include "stats_epilogues.h"
+
+namespace dppo {
+namespace {
+
+DeviceSetup g_setup;
+typedef EpiOut<true, float> EpiOutF32;
+typedef EpiOut<true, uint16_t> EpiOutBf16;
+
+hipError_t allow_all() {
+    hipError_t e = allow_logits<EpiOutF32>();
+    if (e == hipSuccess) e = allow_logits<EpiOutBf16>();
+    return e;
+}
+
+}  // namespace
+
+int mfma_i8_setup(int* compute_units) { return g_setup.run(&allow_all, compute_units); }
+
+void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, hipStream_t st) {
+    if (out_bf16) launch_logits(g, out_epilogue<true, uint16_t>(g, s), st);
+    else launch_logits(g, out_epilogue<true, float>(g, s), st);
+}
+
+}  // namespace dppo

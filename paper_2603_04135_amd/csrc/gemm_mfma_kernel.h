@@ -64,6 +64,26 @@ constexpr int MK = 32;    // k-values of one MFMA
 __device__ __forceinline__ int acc_row(int lane, int j) { return 4 * (lane >> 4) + j; }
 __device__ __forceinline__ int acc_col(int lane) { return lane & 15; }
 
+// Operand type of an epilogue's GEMM. bfloat16 unless the epilogue says Int8: then the 16 bytes of an operand register hold 16
+// 8-bit integers, an MFMA takes 64 k-values and accumulates int32, and everything that moves operands stays as it is, with K, lda
+// and ldb in units of two bytes (both instructions take the k-values of lane group l / 16 from its 16 bytes, in the same order for
+// A and B).
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+struct Bf16Operands {
+    typedef f32x4 acc_t;
+    static __device__ __forceinline__ acc_t mfma(bf16x8 a, bf16x8 b, acc_t c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+    }
+};
+struct Int8Operands {
+    typedef i32x4 acc_t;
+    static __device__ __forceinline__ acc_t mfma(bf16x8 a, bf16x8 b, acc_t c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+    }
+};
+template <class Epi, class = void> struct OperandsOf { typedef Bf16Operands type; };
+template <class Epi> struct OperandsOf<Epi, std::void_t<typename Epi::Int8>> { typedef Int8Operands type; };
+
 #define DPPO_GPTR(p) ((const void __attribute__((address_space(1)))*)(p))
 #define DPPO_LPTR(p) ((void __attribute__((address_space(3)))*)(p))
 
@@ -407,14 +427,15 @@ __global__ __launch_bounds__(Cfg::NT, 2) void gemm_nt_kernel(const uint16_t* __r
         bfr[set][ni] = *reinterpret_cast<const bf16x8*>(st + b_base + ni * MB * ROWB + kc_off);
     };
 
-    f32x4 acc[MI][NI];
+    typedef typename OperandsOf<Epi>::type Operands;
+    typename Operands::acc_t acc[MI][NI];
     auto clear_acc = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[mi][ni][j] = 0.0f;
+                for (int j = 0; j < 4; ++j) acc[mi][ni][j] = 0;
     };
     clear_acc();
 
@@ -515,8 +536,8 @@ __global__ __launch_bounds__(Cfg::NT, 2) void gemm_nt_kernel(const uint16_t* __r
                     for (int q = 0; q < MI * NI; ++q) {
                         const int mi = q / NI, ni = q % NI;
                         acc[mi][ni] = Epi::SWAP
-                            ? __builtin_amdgcn_mfma_f32_16x16x32_bf16(bfr[cur][ni], af[a_slot(mi, cur)], acc[mi][ni], 0, 0, 0)
-                            : __builtin_amdgcn_mfma_f32_16x16x32_bf16(af[a_slot(mi, cur)], bfr[cur][ni], acc[mi][ni], 0, 0, 0);
+                            ? Operands::mfma(bfr[cur][ni], af[a_slot(mi, cur)], acc[mi][ni])
+                            : Operands::mfma(af[a_slot(mi, cur)], bfr[cur][ni], acc[mi][ni]);
                         __builtin_amdgcn_sched_barrier(0);
                         if (reads_here) {
                             if (q == 0) read_a(a_slot(MI - 1, nxt), rsa, read_kk, MI - 1);
@@ -582,7 +603,7 @@ __global__ __launch_bounds__(Cfg::NT, 2) void gemm_nt_kernel(const uint16_t* __r
 // Epilogues
 // ---------------------------------------------------------------------------------------
 // Store of the accumulators. KIND 0 (dW): float output, overwrite or accumulate. KIND 1 (dH):
-// bf16 output, optional row scatter through row_map.
+// bf16 output, optional row scatter through row_map. KIND 2 (dW): bf16 output, overwritten.
 // dW is a read-modify-write of 256 KB per tile. With the MFMA operands swapped (SWAP) a lane's four accumulators are four
 // neighbouring columns, so the tile leaves the registers in 16-byte accesses of 64-byte runs, and 16 old values per lane
 // are in flight together. The LDS stays free for the next tile's first slices (see gemm_nt_kernel). Against a
@@ -599,7 +620,30 @@ struct EpiStore {
 
     template <class Cfg>
     __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
-        if (KIND == 0) {
+        if (KIND == 2 && !partial) {
+            // as below, four neighbouring columns per lane, rounded once; exactly as many stores as with KIND 0
+            const int r0 = c.wave_m * Cfg::WTM + (c.lane & 15), c0 = c.wave_n * Cfg::WTN + 4 * (c.lane >> 4);
+            uint16_t* p = Cb + (size_t)(c.bm0 + r0) * ldc + c.bn0 + c0;
+            const int rows = c.M - c.bm0, cols = c.N - c.bn0;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            auto store = [&](auto full_tag) __attribute__((always_inline)) {
+#pragma unroll
+                for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < Cfg::NI; ++ni)
+                        if (decltype(full_tag)::value || (r0 + mi * MB < rows && c0 + ni * MB < cols)) {
+                            const __bf16 b0 = (__bf16)acc[mi][ni][0], b1 = (__bf16)acc[mi][ni][1];
+                            const __bf16 b2 = (__bf16)acc[mi][ni][2], b3 = (__bf16)acc[mi][ni][3];
+                            const uint32_t lo = (uint32_t)__builtin_bit_cast(uint16_t, b0) | ((uint32_t)__builtin_bit_cast(uint16_t, b1) << 16);
+                            const uint32_t hi = (uint32_t)__builtin_bit_cast(uint16_t, b2) | ((uint32_t)__builtin_bit_cast(uint16_t, b3) << 16);
+                            *reinterpret_cast<uint2*>(p + (size_t)(mi * MB) * ldc + ni * MB) = make_uint2(lo, hi);
+                        }
+            };
+            if (rows >= Cfg::BM && cols >= Cfg::BN) store(std::true_type{});
+            else store(std::false_type{});
+            return;
+        }
+        if (KIND != 1) {
             // accumulator lane: vocabulary row lane % 16, columns 4 (lane / 16) .. + 3 of each block
             typedef float f32x4v __attribute__((ext_vector_type(4)));
             const int64_t ld = partial ? Cfg::BN : ldc;
@@ -691,11 +735,11 @@ struct EpiStore {
             }
     }
 
-    // KIND 0 needs N and ldc to be multiples of 4 and C 16-byte aligned: D is a multiple of 64 and dW 16-byte aligned,
+    // KIND 0 and 2 need N and ldc to be multiples of 4 and C 16-byte aligned: D is a multiple of 64 and dW 16-byte aligned,
     // which the entry points check.
     template <class Cfg>
     static constexpr int lds_bytes() { return 0; }
-    static constexpr bool SWAP = KIND == 0;
+    static constexpr bool SWAP = KIND != 1;
 };
 typedef EpiStore<0> EpiStoreDW;
 typedef EpiStore<1> EpiStoreDH;

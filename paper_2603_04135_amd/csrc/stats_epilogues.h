@@ -1,0 +1,195 @@
+// Epilogues of the vocabulary GEMM (rows = vocabulary entries, columns = tokens) for the token statistics, their gradient and the
+// 8-bit product.
+#pragma once
+#include "gemm_mfma_launch.h"
+#include "stats_internal.h"
+
+namespace dppo {
+namespace mfma {
+
+template <bool I8> struct OperandTag {};
+template <> struct OperandTag<true> { typedef void Int8; };
+
+// The wavefront's accumulators as logits: as they are (bfloat16 operands), or sum * w[v] * h[row] with both scales applied in 32
+// bits, in this order (8-bit operands; the sum itself is exact and is rounded once, to 32 bits).
+template <class Cfg, class Acc>
+__device__ __forceinline__ void to_logits(Acc (&acc)[Cfg::MI][Cfg::NI], f32x4 (&z)[Cfg::MI][Cfg::NI], const TileCtx& c, const OperandScales& s) {
+    if constexpr (std::is_same<Acc, f32x4>::value) {
+#pragma unroll
+        for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < Cfg::NI; ++ni) z[mi][ni] = acc[mi][ni];
+    } else {
+        float h[Cfg::NI];
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            const int n = c.n0 + ni * MB + acc_col(c.lane);
+            int row = n < c.N ? n : c.N - 1;
+            if (s.map) row = s.map[row];
+            h[ni] = s.h[row < 0 ? 0 : row < s.rows ? row : s.rows - 1];
+        }
+#pragma unroll
+        for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int v = c.m0 + mi * MB + acc_row(c.lane, j);
+                const float w = s.w[v < c.M ? v : c.M - 1];
+#pragma unroll
+                for (int ni = 0; ni < Cfg::NI; ++ni) z[mi][ni][j] = (float)acc[mi][ni][j] * w * h[ni];
+            }
+    }
+}
+
+// Stores the logits, row-major by token: C[n, v]. A lane's four accumulators are four neighbouring vocabulary entries of one token,
+// one store where the pitch allows it.
+template <bool I8, class Out>
+struct EpiOut : OperandTag<I8> {
+    Out* C; int64_t ldc; int vec;          // vec: whole groups of four are aligned
+    OperandScales scales;
+
+    __device__ __forceinline__ void look_up(int, int) const {}
+    template <class Cfg, class Acc>
+    __device__ __forceinline__ void run(Acc (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        f32x4 z[Cfg::MI][Cfg::NI];
+        to_logits<Cfg>(acc, z, c, scales);
+        auto store = [&](auto full_tag) __attribute__((always_inline)) {
+            constexpr bool FULL = decltype(full_tag)::value;
+#pragma unroll
+            for (int ni = 0; ni < Cfg::NI; ++ni) {
+                const int n = c.n0 + ni * MB + acc_col(c.lane);
+                if (!FULL && n >= c.N) continue;
+                Out* dst = C + (size_t)n * ldc + c.m0 + acc_row(c.lane, 0);
+#pragma unroll
+                for (int mi = 0; mi < Cfg::MI; ++mi) {
+                    const f32x4 v = z[mi][ni];
+                    if (FULL) {
+                        if constexpr (sizeof(Out) == 4) {
+                            *reinterpret_cast<f32x4*>(dst + mi * MB) = v;
+                        } else {
+                            const __bf16 b0 = (__bf16)v[0], b1 = (__bf16)v[1], b2 = (__bf16)v[2], b3 = (__bf16)v[3];
+                            const uint32_t lo = (uint32_t)__builtin_bit_cast(uint16_t, b0) | ((uint32_t)__builtin_bit_cast(uint16_t, b1) << 16);
+                            const uint32_t hi = (uint32_t)__builtin_bit_cast(uint16_t, b2) | ((uint32_t)__builtin_bit_cast(uint16_t, b3) << 16);
+                            *reinterpret_cast<uint2*>(dst + mi * MB) = make_uint2(lo, hi);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if (c.m0 + mi * MB + acc_row(c.lane, j) >= c.M) continue;
+                            if constexpr (sizeof(Out) == 4) {
+                                dst[mi * MB + j] = v[j];
+                            } else {
+                                const __bf16 b = (__bf16)v[j];
+                                dst[mi * MB + j] = __builtin_bit_cast(uint16_t, b);
+                            }
+                        }
+                    }
+                }
+            }
+        };
+        if (vec && c.bm0 + Cfg::BM <= c.M && c.bn0 + Cfg::BN <= c.N) store(std::true_type{});
+        else store(std::false_type{});
+    }
+
+    template <class Cfg>
+    static constexpr int lds_bytes() { return 0; }
+    static constexpr bool SWAP = false;
+};
+
+// Gradient entries of the statistics straight from the logits (see grad_entry), staged through LDS as [token][vocabulary row] and
+// stored to the blocked chunk. Everything, the target's entry too, comes from the accumulators that the forward pass summed the
+// same way.
+struct EpiStatsGrad {
+    const int32_t* y; StatsGrad grad; int64_t n0; int n_c;
+    uint16_t* G; int64_t ldg; int V;
+
+    template <class Cfg>
+    __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        constexpr int ZPITCH = StagedStore<Cfg>::ZPITCH;
+        auto body = [&](auto full_tag) __attribute__((always_inline)) {
+            constexpr bool FULL = decltype(full_tag)::value;
+#pragma unroll
+            for (int ni = 0; ni < Cfg::NI; ++ni) {
+                const int tok = c.wave_n * Cfg::WTN + ni * MB + acc_col(c.lane);
+                const int n = c.bn0 + tok;
+                TokenGrad t{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                int at = -1;                                        // target among the wavefront's rows
+                if (n < n_c) {
+                    t = load_grad(grad, n0 + n);
+                    at = y[n] - (c.bm0 + c.wave_m * Cfg::WTM);
+                }
+#pragma unroll
+                for (int mi = 0; mi < Cfg::MI; ++mi) {
+                    const int vloc = c.wave_m * Cfg::WTM + mi * MB + acc_row(c.lane, 0);
+                    bf16x4 h;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float lp = acc[mi][ni][q] - t.lse;
+                        float g = grad_entry(t, lp, __builtin_amdgcn_exp2f(lp * LOG2E), false);
+                        // (a padding token's row of zeros times a weight of -infinity is NaN, which dW would sum)
+                        g = n < n_c && (FULL || c.bm0 + vloc + q < V) ? g : 0.0f;
+                        const __bf16 b = (__bf16)g;   // scalar copy: reading h[q] back right after writing it miscompiles
+                        h[q] = b;
+                    }
+                    *reinterpret_cast<bf16x4*>(c.smem + tok * ZPITCH + vloc * 2) = h;
+                }
+                if (!__any(at >= 0 && at < Cfg::WTM)) continue;
+#pragma unroll
+                for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        if (at != mi * MB + acc_row(c.lane, q)) continue;
+                        const float lp = acc[mi][ni][q] - t.lse;
+                        const __bf16 b = (__bf16)grad_entry(t, lp, __builtin_amdgcn_exp2f(lp * LOG2E), true);
+                        *reinterpret_cast<__bf16*>(c.smem + tok * ZPITCH + (c.wave_m * Cfg::WTM + at) * 2) = b;
+                    }
+            }
+        };
+        if (c.bm0 + Cfg::BM <= V) body(std::true_type{});
+        else body(std::false_type{});
+        __syncthreads();
+        const StagedStore<Cfg> staged(c, G, ldg);
+#pragma unroll
+        for (int b = 0; b < Cfg::BN / BLK_R; ++b)
+#pragma unroll
+            for (int p = 0; p < BLK_R / MB; ++p) staged.pass(b, p);
+    }
+
+    template <class Cfg>
+    static constexpr int lds_bytes() { return Cfg::BN * (Cfg::BM * 2 + 16); }
+    static constexpr bool SWAP = false;
+};
+
+}  // namespace mfma
+
+namespace {
+// The tile of the vocabulary GEMM by the number of tokens, as for the log-probabilities alone (see CfgFew): up to 192 tokens
+// columns that read the tokens' rows of H where they lie, through the map. Beyond, the rows are contiguous.
+template <class Epi>
+void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st) {
+    auto mapped = [&](auto cfg) {
+        launch<decltype(cfg), A_ROWS, WG_ROUNDS, B_MAP>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, 0, -1, 1, -1, (int)g.h_rows, 0, g.map, 0);
+    };
+    if (g.n <= 96) mapped(CfgFew<96>{});
+    else if (g.n <= 128) mapped(CfgFew<128>{});
+    else if (g.n <= STATS_MAP_TOKENS) mapped(CfgBig192{});
+    else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st);
+}
+template <class Epi>
+hipError_t allow_logits() {
+    hipError_t e = allow_lds<CfgFew<96>, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
+    if (e == hipSuccess) e = allow_lds<CfgFew<128>, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
+    if (e == hipSuccess) e = allow_lds<CfgBig192, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
+    if (e == hipSuccess) e = allow_lds<CfgBig, Epi>();
+    return e;
+}
+template <bool I8, class Out>
+EpiOut<I8, Out> out_epilogue(const LogitsOut& g, const OperandScales& s) {
+    EpiOut<I8, Out> e;
+    e.C = reinterpret_cast<Out*>(g.C);
+    e.ldc = g.ldc;
+    e.vec = g.ldc % 4 == 0 && reinterpret_cast<uintptr_t>(g.C) % (4 * sizeof(Out)) == 0;
+    e.scales = s;
+    return e;
+}
+}  // namespace
+}  // namespace dppo

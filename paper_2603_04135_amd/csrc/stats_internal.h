@@ -1,0 +1,82 @@
+// Internal declarations of the token statistics, their gradient and the 8-bit operators.
+#pragma once
+#include "dppo_internal.h"
+
+namespace dppo {
+
+// ---- token statistics (stats_rows.hip) ---------------------------------------
+struct StatsOut {
+    float* lse; float* entropy; float* logp;     // each may be NULL
+    int32_t* top_ids; float* top_logp; int32_t top_k;
+};
+// Rows of logits cut into parts: per (token, part) the statistics {max, sum, dev, -} and the top_k keys.
+struct PartialStats {
+    float4* stats; uint64_t* keys; int32_t parts;
+};
+// Parts that the rows of n_c tokens are cut into.
+int stats_row_parts(int32_t n_c, int32_t V, int cus);
+void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
+
+// Copies of the tokens' rows (row_bytes: a multiple of 4; below 16-byte alignment they are taken for float32), their targets (-1 without ids), clamped rows and scales;
+// any of the outputs may be NULL.
+struct GatherRows {
+    TokenArgs tokens; size_t row_bytes; const float* scale;
+    void* out; int32_t* y; int32_t* rowc; float* scale_out;
+};
+void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st);
+
+// ---- gradient of the statistics ----------------------------------------------
+// Incoming gradients (each may be NULL = 0) and the forward's results, per loss token.
+struct StatsGrad {
+    const float* g_logp; const float* g_lse; const float* g_entropy;
+    const float* lse; const float* entropy;
+};
+struct TokenGrad { float lse, ent, gl, ge, gs, c; };
+__device__ __forceinline__ TokenGrad load_grad(const StatsGrad& g, int64_t n) {
+    TokenGrad t;
+    t.lse = g.lse[n];
+    t.gl = g.g_logp ? g.g_logp[n] : 0.0f;
+    t.gs = g.g_lse ? g.g_lse[n] : 0.0f;
+    t.ge = g.g_entropy ? g.g_entropy[n] : 0.0f;
+    t.ent = g.g_entropy ? g.entropy[n] : 0.0f;
+    t.c = t.gs - t.gl - t.ge * t.ent;
+    return t;
+}
+// Gradient entry of a logit of log-probability lp and probability p. lp is cut where p is 0 in 32 bits (0, not 0 * infinity); the
+// target's 1 - p is formed as such: p near 1 must cancel against the 1 before anything is added.
+__device__ __forceinline__ float grad_entry(const TokenGrad& t, float lp, float p, bool target) {
+    const float cut = fmaxf(lp, -150.0f);
+    return target ? fmaf(t.gl, 1.0f - p, p * (t.gs - t.ge * (cut + t.ent))) : p * fmaf(-t.ge, cut, t.c);
+}
+void launch_stats_grad_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const StatsGrad& g, ChunkView cv, hipStream_t st);
+// dst (bfloat16) = src, n a multiple of 4, both 16-byte aligned.
+void launch_to_bf16(const float* src, void* dst, size_t n, hipStream_t st);
+
+// ---- GEMMs (gemm_stats.hip, gemm_i8.hip) --------------------------------------
+// Scales of 8-bit operands: logit = sum * w[v] * h[row]; row = map[n] clamped to `rows` (map NULL: n).
+struct OperandScales {
+    const float* w; const float* h; const int32_t* map; int32_t rows;
+};
+// Logits of n tokens, C[n, V] = H W^T with pitch ldc. k2: bytes of an operand row / 2 (a multiple of 64). Row n of the tokens is row
+// map[n] (clamped to h_rows) of H, or n where map is NULL; a map needs n <= STATS_MAP_TOKENS.
+struct LogitsOut {
+    const void* W; int32_t V; int32_t k2;
+    const void* H; int64_t h_rows; const int32_t* map; int32_t n;
+    void* C; int64_t ldc;
+};
+constexpr int32_t STATS_MAP_TOKENS = 192;
+int mfma_stats_setup(int* compute_units);
+int mfma_i8_setup(int* compute_units);
+void launch_logits_bf16(const LogitsOut& g, hipStream_t st);                                       // C float32
+void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, hipStream_t st);  // C float32 or bfloat16
+// bfloat16 gradient entries of a chunk in the blocked layout (see launch_mfma_logits_grad).
+void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc, ChunkView cv, const int32_t* y, const StatsGrad& g, void* G,
+                            int32_t Vp, hipStream_t st);
+// launch_mfma_dw with a bfloat16 result, overwritten.
+void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
+                         hipStream_t st);
+
+// ---- 8-bit rows (quantize.hip) -------------------------------------------------
+void launch_quantize_rows(int dtype, const void* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float* scale, hipStream_t st);
+
+}  // namespace dppo
