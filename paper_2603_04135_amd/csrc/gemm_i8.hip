@@ -11,6 +11,8 @@ typedef EpiOut<true, uint16_t> EpiOutBf16;
 hipError_t allow_all() {
     hipError_t e = allow_logits<EpiOutF32>();
     if (e == hipSuccess) e = allow_logits<EpiOutBf16>();
+    if (e == hipSuccess) e = allow_logits<EpiStats<true, false>>();
+    if (e == hipSuccess) e = allow_logits<EpiStats<true, true>>();
     return e;
 }
 
@@ -21,6 +23,10 @@ int mfma_i8_setup(int* compute_units) { return g_setup.run(&allow_all, compute_u
 void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, hipStream_t st) {
     if (out_bf16) launch_logits(g, out_epilogue<true, uint16_t>(g, s), st);
     else launch_logits(g, out_epilogue<true, float>(g, s), st);
+}
+
+void launch_stats_i8(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st) {
+    launch_stats_tiles<true>(g, s, t, st);
 }
 
 }  // namespace dppo

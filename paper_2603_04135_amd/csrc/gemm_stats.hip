@@ -6,10 +6,10 @@ namespace {
 
 DeviceSetup g_setup;
 typedef EpiStore<2> EpiStoreDW16;
-typedef EpiOut<false, float> EpiLogitsOut;
 
 hipError_t allow_all() {
-    hipError_t e = allow_logits<EpiLogitsOut>();
+    hipError_t e = allow_logits<EpiStats<false, false>>();
+    if (e == hipSuccess) e = allow_logits<EpiStats<false, true>>();
     if (e == hipSuccess) e = allow_lds<CfgBig, EpiStatsGrad>();
     if (e == hipSuccess) e = allow_lds<CfgGrad, EpiStoreDW16, A_BLK_KM, WG_RANGES, B_BLK>();
     return e;
@@ -19,8 +19,8 @@ hipError_t allow_all() {
 
 int mfma_stats_setup(int* compute_units) { return g_setup.run(&allow_all, compute_units); }
 
-void launch_logits_bf16(const LogitsOut& g, hipStream_t st) {
-    launch_logits(g, out_epilogue<false, float>(g, OperandScales{nullptr, nullptr, nullptr, 0}), st);
+void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, hipStream_t st) {
+    launch_stats_tiles<false>(g, OperandScales{nullptr, nullptr, nullptr, 0}, t, st);
 }
 
 void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc, ChunkView cv, const int32_t* y, const StatsGrad& g, void* G,

@@ -17,7 +17,7 @@ constexpr size_t LOGITS_CHUNK_BYTES = (size_t)8 << 30;
 struct Regions {                            // offsets into the workspace
     int32_t Vp, n_cp;
     size_t row_bytes;
-    size_t o_hc, o_scale, o_z, o_pstats, o_pkeys;                                        // forward
+    size_t o_hc, o_scale, o_z, o_pstats, o_pkeys, o_ms, o_dev, o_zy;                     // forward
     size_t o_wt, o_dwpart, o_dwacc, o_hct, o_fpart, o_y, o_rowc;                         // backward
     bool direct_w;
     int f32_parts;
@@ -38,9 +38,15 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
     if (what == FORWARD) {
         r.o_hc = take(s.dtype == F32 ? 0 : n * r.row_bytes);
         r.o_scale = take(s.dtype == I8 ? n * 4 : 0);
-        r.o_z = take(n * r.Vp * 4);
-        // rows are cut into parts only where there are fewer than 4 per compute unit: at most 8 * DEFAULT_CUS parts in all
-        const size_t parts = 8 * DEFAULT_CUS;
+        r.o_z = take(s.dtype == F32 || top_k > 0 ? n * r.Vp * 4 : 0);
+        // (128-row tiles have at most 128 tokens: no more pairs than 256-row tiles of 256)
+        const size_t pairs = s.dtype == F32 ? 0 : n * mfma_logits_row_tiles(s.V);
+        r.o_ms = take(pairs * sizeof(float2));
+        r.o_dev = take(pairs * 4);
+        r.o_zy = take(s.dtype == F32 ? 0 : n * 4);
+        r.o_y = take(s.dtype == F32 ? 0 : n * 4);
+        // float32: rows are cut into parts only where there are fewer than 4 per compute unit: at most 8 * DEFAULT_CUS parts in all
+        const size_t parts = s.dtype == F32 ? 8 * DEFAULT_CUS : 0;
         r.o_pstats = take(parts * sizeof(float4));
         r.o_pkeys = take(parts * top_k * sizeof(uint64_t));
         r.total = off;
@@ -182,32 +188,41 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         const ChunkView cv = view(n0, s.N, r.n_cp);
         const int32_t* map = loss_pos ? loss_pos + n0 : nullptr;
         if (s.dtype == F32) {
-            StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
             const float* A = reinterpret_cast<const float*>(H) + (map ? 0 : (size_t)n0 * s.D);
             GemmF32 g{A, s.D, 0, reinterpret_cast<const float*>(W), s.D, 0, cv.n_c, s.V, s.D, Z, r.Vp, 0, nullptr, nullptr, 0,
                       map, (int32_t)s.T};
             launch_gemm_f32(g, cus, st);
-        } else {
-            // rows in order are read where they are; rows through loss_pos too while the GEMM's columns take a map
-            const char* rows = reinterpret_cast<const char*>(H) + (map ? 0 : (size_t)n0 * r.row_bytes);
-            LogitsOut g{W, s.V, (int32_t)(r.row_bytes / 2), rows, map ? s.T : (int64_t)cv.n_c, map, cv.n_c, Z, r.Vp};
-            OperandScales sc{w_scale, h_scale ? h_scale + (map ? 0 : n0) : nullptr, map, (int32_t)g.h_rows};
-            if (map && cv.n_c > STATS_MAP_TOKENS) {
-                StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-                float* scale = reinterpret_cast<float*>(w + r.o_scale);
-                GatherRows gr{tokens, r.row_bytes, h_scale, w + r.o_hc, nullptr, nullptr, s.dtype == I8 ? scale : nullptr};
-                launch_stats_gather(gr, cv, st);
-                g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr;
-                sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c;
-            }
+            StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
+            PartialStats partial{reinterpret_cast<float4*>(w + r.o_pstats), reinterpret_cast<uint64_t*>(w + r.o_pkeys),
+                                 stats_row_parts(cv.n_c, s.V, DEFAULT_CUS)};
+            launch_stats_rows(Z, r.Vp, tokens, out, cv, partial, st);
+            continue;
+        }
+        // Few tokens: the GEMM's columns read the rows through loss_pos, its epilogue looks the targets up. Many: both are gathered first.
+        const bool few = cv.n_c <= STATS_MAP_TOKENS;
+        const char* rows = reinterpret_cast<const char*>(H) + (map ? 0 : (size_t)n0 * r.row_bytes);
+        LogitsOut g{W, s.V, (int32_t)(r.row_bytes / 2), rows, map ? s.T : (int64_t)cv.n_c, map, cv.n_c, top_k > 0 ? Z : nullptr, r.Vp};
+        OperandScales sc{w_scale, h_scale ? h_scale + (map ? 0 : n0) : nullptr, map, (int32_t)g.h_rows};
+        int32_t* y = reinterpret_cast<int32_t*>(w + r.o_y);
+        if (!few && (map || logp)) {
+            StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
+            float* scale = reinterpret_cast<float*>(w + r.o_scale);
+            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr};
+            launch_stats_gather(gr, cv, st);
+            if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
+            if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
+        }
+        StatsTiles t{{reinterpret_cast<float2*>(w + r.o_ms), reinterpret_cast<float*>(w + r.o_dev),
+                      logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, few ? cv.n_c : cv.n_cp},
+                     tokens, few ? nullptr : y, cv};
+        {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
-            if (s.dtype == BF16) launch_logits_bf16(g, st);
-            else launch_logits_i8(g, sc, false, st);
+            if (s.dtype == BF16) launch_stats_bf16(g, t, st);
+            else launch_stats_i8(g, sc, t, st);
         }
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        PartialStats partial{reinterpret_cast<float4*>(w + r.o_pstats), reinterpret_cast<uint64_t*>(w + r.o_pkeys),
-                             stats_row_parts(cv.n_c, s.V, DEFAULT_CUS)};
-        launch_stats_rows(Z, r.Vp, tokens, out, cv, partial, st);
+        const int32_t tile = logits_tile_rows(cv.n_c);
+        launch_stats_join(t.part, (int32_t)ceil_div(s.V, tile), tile, Z, r.Vp, tokens, few, out, cv, st);
     }
     return check_launch("dppo_token_stats");
 }

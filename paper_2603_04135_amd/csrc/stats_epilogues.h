@@ -95,6 +95,113 @@ struct EpiOut : OperandTag<I8> {
     static constexpr bool SWAP = false;
 };
 
+// Softmax statistics of every token over the tile's vocabulary rows, {max, sum exp(z - max)} and sum (z - max) exp(z - max) (see
+// Stats), in registers and combined across the wavefronts through LDS; the target's logit from the accumulator that holds it; with
+// STORE the logits themselves, row-major by token, for the top alternatives.
+template <bool I8, bool STORE>
+struct EpiStats : OperandTag<I8> {
+    StatsPart part;
+    OperandScales scales;
+    // y[n]: targets looked up before, or NULL: from tokens.ids (NULL: no targets)
+    TokenArgs tokens; const int32_t* y; int64_t n0; int n_c;
+    float* Z; int64_t ldz;
+
+    __device__ __forceinline__ void look_up(int, int) const {}
+    template <class Cfg, class Acc>
+    __device__ __forceinline__ void run(Acc (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        constexpr int MI = Cfg::MI, NI = Cfg::NI;
+        const float NEG_INF = -__builtin_inff();
+        f32x4 z[MI][NI];
+        to_logits<Cfg>(acc, z, c, scales);
+        if (STORE) {
+            // whole tiles, the padding of the vocabulary too (the pitch holds it)
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                const int n = c.n0 + ni * MB + acc_col(c.lane);
+                if (n >= n_c) continue;
+                float* dst = Z + (size_t)n * ldz + c.m0 + acc_row(c.lane, 0);
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi) *reinterpret_cast<f32x4*>(dst + mi * MB) = z[mi][ni];
+            }
+        }
+        float3* red = reinterpret_cast<float3*>(c.smem);
+        auto reduce = [&](auto full_tag) __attribute__((always_inline)) {
+            constexpr bool FULL = decltype(full_tag)::value;
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                float m = NEG_INF;
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (!FULL && c.m0 + mi * MB + acc_row(c.lane, j) >= c.M) z[mi][ni][j] = NEG_INF;
+                        m = fmaxf(m, z[mi][ni][j]);
+                    }
+                m = fmaxf(m, __shfl_xor(m, 16, 64));
+                m = fmaxf(m, __shfl_xor(m, 32, 64));
+                const float ref = m == NEG_INF ? 0.0f : m;
+                float sum = 0.0f, dev = 0.0f;
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float d = z[mi][ni][j] - ref, e = __builtin_amdgcn_exp2f(d * LOG2E);
+                        sum += e;
+                        dev = fmaf(fmaxf(d, DEV_MIN), e, dev);
+                    }
+                sum += __shfl_xor(sum, 16, 64);
+                sum += __shfl_xor(sum, 32, 64);
+                dev += __shfl_xor(dev, 16, 64);
+                dev += __shfl_xor(dev, 32, 64);
+                if (c.lane < MB) red[c.wave_m * Cfg::BN + c.wave_n * Cfg::WTN + ni * MB + c.lane] = make_float3(m, sum, dev);
+            }
+        };
+        if (c.bm0 + Cfg::BM <= c.M) reduce(std::true_type{});
+        else reduce(std::false_type{});
+        if (part.zy) {
+#pragma unroll
+            for (int ni = 0; ni < NI; ++ni) {
+                const int n = c.n0 + ni * MB + acc_col(c.lane);
+                int at = -1;                                        // target among the wavefront's rows
+                if (n < n_c) {
+                    int32_t t;
+                    if (y) {
+                        t = y[n];
+                    } else {
+                        int64_t row;
+                        locate_token(tokens.ids, tokens.loss_pos, tokens.T, tokens.V, n0 + n, row, t);
+                    }
+                    at = t - c.m0;
+                }
+                if (!__any(at >= 0 && at < Cfg::WTM)) continue;
+#pragma unroll
+                for (int mi = 0; mi < MI; ++mi)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (at == mi * MB + acc_row(c.lane, j)) part.zy[n] = z[mi][ni][j];
+            }
+        }
+        __syncthreads();
+        for (int t = c.tid; t < Cfg::BN; t += Cfg::NT) {
+            const int n = c.bn0 + t;
+            if (n >= n_c) continue;
+            Stats s = no_stats();
+#pragma unroll
+            for (int w = 0; w < Cfg::WGM; ++w) {
+                const float3 r = red[w * Cfg::BN + t];
+                s = join(s, Stats{r.x, r.y, r.z});
+            }
+            const size_t at = (size_t)c.tm * part.pitch + n;
+            part.ms[at] = make_float2(s.m, s.sum);
+            part.dev[at] = s.dev;
+        }
+    }
+
+    template <class Cfg>
+    static constexpr int lds_bytes() { return Cfg::WGM * Cfg::BN * 12; }
+    static constexpr bool SWAP = false;
+};
+
 // Gradient entries of the statistics straight from the logits (see grad_entry), staged through LDS as [token][vocabulary row] and
 // stored to the blocked chunk. Everything, the target's entry too, comes from the accumulators that the forward pass summed the
 // same way.
@@ -181,6 +288,16 @@ hipError_t allow_logits() {
     if (e == hipSuccess) e = allow_lds<CfgBig192, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
     if (e == hipSuccess) e = allow_lds<CfgBig, Epi>();
     return e;
+}
+template <bool I8>
+void launch_stats_tiles(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st) {
+    auto go = [&](auto e) {
+        e.part = t.part; e.scales = s; e.tokens = t.tokens; e.y = t.y; e.n0 = t.cv.n0; e.n_c = t.cv.n_c;
+        e.Z = reinterpret_cast<float*>(g.C); e.ldz = g.ldc;
+        launch_logits(g, e, st);
+    };
+    if (g.C) go(EpiStats<I8, true>{});
+    else go(EpiStats<I8, false>{});
 }
 template <bool I8, class Out>
 EpiOut<I8, Out> out_epilogue(const LogitsOut& g, const OperandScales& s) {

@@ -9,6 +9,19 @@ struct StatsOut {
     float* lse; float* entropy; float* logp;     // each may be NULL
     int32_t* top_ids; float* top_logp; int32_t top_k;
 };
+// Statistics of a set of logits against its maximum m: sum = sum exp(z - m), dev = sum (z - m) exp(z - m). With them
+// lse = m + log(sum) and the entropy -sum p log p = log(sum) - dev / sum, in which nothing of the size of the logits cancels.
+struct Stats { float m, sum, dev; };
+// exp() is 0 in 32 bits below -104: differences are cut at -150 where they are multiplied by it, so that a logit at -infinity (or
+// at the type's lowest value, whose difference overflows) adds 0 and not 0 * infinity.
+constexpr float DEV_MIN = -150.0f;
+__device__ __forceinline__ Stats no_stats() { return Stats{-__builtin_inff(), 0.0f, 0.0f}; }
+__device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
+    const float m = fmaxf(a.m, b.m), ref = m == -__builtin_inff() ? 0.0f : m;
+    const float da = a.m - ref, db = b.m - ref, ea = expf(da), eb = expf(db);
+    return Stats{m, a.sum * ea + b.sum * eb,
+                 ea * (a.dev + fmaxf(da, DEV_MIN) * a.sum) + eb * (b.dev + fmaxf(db, DEV_MIN) * b.sum)};
+}
 // Rows of logits cut into parts: per (token, part) the statistics {max, sum, dev, -} and the top_k keys.
 struct PartialStats {
     float4* stats; uint64_t* keys; int32_t parts;
@@ -16,6 +29,12 @@ struct PartialStats {
 // Parts that the rows of n_c tokens are cut into.
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
+
+// Per-tile statistics of the vocabulary GEMM: {max, sum} and dev of row tile t and token n at [t * pitch + n]; zy[n]: target logits (or NULL).
+struct StatsPart { float2* ms; float* dev; float* zy; int32_t pitch; };
+// Joins a token's tiles (tile: rows of one) and picks the top alternatives from the stored logits of the tiles that can hold them.
+void launch_stats_join(const StatsPart& part, int32_t tiles, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+                       const StatsOut& o, ChunkView cv, hipStream_t st);
 
 // Copies of the tokens' rows (row_bytes: a multiple of 4; below 16-byte alignment they are taken for float32), their targets (-1 without ids), clamped rows and scales;
 // any of the outputs may be NULL.
@@ -65,9 +84,14 @@ struct LogitsOut {
     void* C; int64_t ldc;
 };
 constexpr int32_t STATS_MAP_TOKENS = 192;
+// Vocabulary rows of a tile for n tokens.
+inline int32_t logits_tile_rows(int32_t n) { return n <= 128 ? 128 : 256; }
+// The same GEMM with the statistics in its epilogue (C NULL: the logits are not stored; otherwise ldc holds whole tiles).
+struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkView cv; };
 int mfma_stats_setup(int* compute_units);
 int mfma_i8_setup(int* compute_units);
-void launch_logits_bf16(const LogitsOut& g, hipStream_t st);                                       // C float32
+void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, hipStream_t st);
+void launch_stats_i8(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st);
 void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, hipStream_t st);  // C float32 or bfloat16
 // bfloat16 gradient entries of a chunk in the blocked layout (see launch_mfma_logits_grad).
 void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc, ChunkView cv, const int32_t* y, const StatsGrad& g, void* G,

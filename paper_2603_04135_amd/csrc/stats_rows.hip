@@ -1,5 +1,8 @@
 // Kernels around the logits GEMMs of dppo_token_stats and dppo_token_stats_bwd: softmax statistics and top alternatives of stored
 // logits, gathering of rows, gradient entries of the float32 path.
+#include <type_traits>
+
+#include "api_internal.h"
 #include "stats_internal.h"
 #include "top_list.h"
 #include "token_rows.h"
@@ -7,21 +10,6 @@
 namespace dppo {
 namespace {
 
-// Statistics of a set of logits against its maximum m: sum = sum exp(z - m), dev = sum (z - m) exp(z - m). With them
-// lse = m + log(sum) and the entropy -sum p log p = log(sum) - dev / sum, in which nothing of the size of the logits cancels.
-struct Stats { float m, sum, dev; };
-
-// exp() is 0 in 32 bits below -104: differences are cut at -150 where they are multiplied by it, so that a logit at -infinity (or
-// at the type's lowest value, whose difference overflows) adds 0 and not 0 * infinity.
-constexpr float DEV_MIN = -150.0f;
-
-__device__ __forceinline__ Stats no_stats() { return Stats{-__builtin_inff(), 0.0f, 0.0f}; }
-__device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
-    const float m = fmaxf(a.m, b.m), ref = m == -__builtin_inff() ? 0.0f : m;
-    const float da = a.m - ref, db = b.m - ref, ea = expf(da), eb = expf(db);
-    return Stats{m, a.sum * ea + b.sum * eb,
-                 ea * (a.dev + fmaxf(da, DEV_MIN) * a.sum) + eb * (b.dev + fmaxf(db, DEV_MIN) * b.sum)};
-}
 __device__ __forceinline__ Stats join_lanes(Stats s) {
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1)
@@ -41,6 +29,20 @@ __device__ __forceinline__ void write_top(const StatsOut& o, int64_t n, const St
     const float lse = s.m + logf(s.sum);
     o.top_ids[n * o.top_k + lane] = (int32_t)top_index(top.entry);
     o.top_logp[n * o.top_k + lane] = top_value(top.entry) - lse;
+}
+
+// ORs what is wrong with loss token i's position or target into *a.status.
+__device__ __forceinline__ void report_token(const TokenArgs& a, int64_t i) {
+    int64_t row;
+    int32_t target;
+    int flags = 0;
+    if (a.ids) {
+        flags = locate_token(a.ids, a.loss_pos, a.T, a.V, i, row, target);
+    } else if (a.loss_pos) {
+        row = a.loss_pos[i];
+        if (row < 0 || row >= a.T) flags = DPPO_HEAD_BAD_POSITION;
+    }
+    if (flags != 0) atomicOr(a.status, flags);
 }
 
 // One workgroup per token and part of its row of stored logits (pitch a multiple of 256; columns from V on hold anything): one pass
@@ -96,7 +98,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
                 const int i = i0 + u * ROWS_THREADS + lane;
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
-                    top.offer(i < hi && i * 4 + q < a.V ? top_key(x[u][q], (uint32_t)(i * 4 + q)) : 0, o.top_k);
+                    top.offer(i < hi && i * 4 + q < a.V ? top_key(x[u][q], (uint32_t)(i * 4 + q)) : 0, o.top_k, lane);
             }
         }
     }
@@ -107,7 +109,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
     if (wave != 0) return;
     for (int w = 1; w < ROWS_WAVES; ++w) s = join(s, red[w]);
     if (TOP) {
-        for (int w = 1; w < ROWS_WAVES; ++w) top.offer(lists[w][lane], o.top_k);
+        for (int w = 1; w < ROWS_WAVES; ++w) top.merge(lists[w][lane], lane);
     }
     const int64_t gi = cv.n0 + n;
     if (partial.parts > 1) {
@@ -120,13 +122,10 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
     if (a.ids) {
         int64_t row;
         int32_t target;
-        const int flags = locate_token(a.ids, a.loss_pos, a.T, a.V, gi, row, target);
-        if (flags != 0 && a.status != nullptr && lane == 0) atomicOr(a.status, flags);
+        locate_token(a.ids, a.loss_pos, a.T, a.V, gi, row, target);
         zy = z[target];
-    } else if (a.loss_pos && a.status != nullptr && lane == 0) {
-        const int64_t row = a.loss_pos[gi];
-        if (row < 0 || row >= a.T) atomicOr(a.status, DPPO_HEAD_BAD_POSITION);
     }
+    if (a.status != nullptr && lane == 0) report_token(a, gi);
     if (lane == 0) write_token(o, gi, s, zy);
     if (TOP) write_top(o, gi, s, top, lane);
 }
@@ -146,22 +145,130 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
     TopList top;
     if (TOP) {
         const int entries = partial.parts * o.top_k;
-        for (int i = 0; i < entries; i += 64) top.offer(i + lane < entries ? partial.keys[at * o.top_k + i + lane] : 0, o.top_k);
+        for (int i = 0; i < entries; i += 64) top.offer(i + lane < entries ? partial.keys[at * o.top_k + i + lane] : 0, o.top_k, lane);
     }
     const int64_t gi = cv.n0 + n;
     float zy = 0.0f;
     if (a.ids) {
         int64_t row;
         int32_t target;
-        const int flags = locate_token(a.ids, a.loss_pos, a.T, a.V, gi, row, target);
-        if (flags != 0 && a.status != nullptr && lane == 0) atomicOr(a.status, flags);
+        locate_token(a.ids, a.loss_pos, a.T, a.V, gi, row, target);
         zy = Z[(size_t)n * ldz + target];
-    } else if (a.loss_pos && a.status != nullptr && lane == 0) {
-        const int64_t row = a.loss_pos[gi];
-        if (row < 0 || row >= a.T) atomicOr(a.status, DPPO_HEAD_BAD_POSITION);
     }
+    if (a.status != nullptr && lane == 0) report_token(a, gi);
     if (lane == 0) write_token(o, gi, s, zy);
     if (TOP) write_top(o, gi, s, top, lane);
+}
+
+// Joins the per-tile statistics of TOK tokens per workgroup, and picks their top alternatives. The k largest logits of a token lie in
+// the k tiles with the largest maxima (in the order of maximum, then tile: every tile ahead of another one holds a logit that is ahead
+// of all of the other's), so that of the stored logits only those tiles are read: k KB of a row of V.
+// The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
+// list the tiles and their logits.
+constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 4;
+template <int TOK, bool TOP>
+__global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tiles, int32_t tile, const float* __restrict__ Z,
+                                                                  int64_t ldz, TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
+    constexpr int GROUPS = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;      // lane groups of the tiles; wavefronts per token
+    constexpr int ROW = TOK == 1 ? 1 : TOK + 1, BLOCK = JOIN_MAXIMA / TOK;  // maxima in LDS: tiles of a block, their row pitch
+    __shared__ float maxima[TOP ? BLOCK * ROW : 1];
+    __shared__ Stats red[JOIN_WAVES][TOK];
+    __shared__ Stats fin[TOK];
+    __shared__ uint64_t lists[TOP && WPT > 1 ? JOIN_WAVES : 1][TOP_MAX];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tok = tid % TOK, group = tid / TOK, n = blockIdx.x * TOK + tok;
+    const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
+    const Stats none = no_stats();
+    Stats s = none;
+    TopList top;
+    for (int b0 = 0; b0 < tiles; b0 += BLOCK) {
+        const int b1 = tiles - b0 < BLOCK ? tiles : b0 + BLOCK;
+        if (TOP && b0 > 0) __syncthreads();
+        if (n < cv.n_c) {
+            for (int t0 = b0 + group; t0 < b1; t0 += GROUPS * JOIN_UNROLL) {
+                Stats p[JOIN_UNROLL];
+#pragma unroll
+                for (int u = 0; u < JOIN_UNROLL; ++u) {
+                    const int t = t0 + u * GROUPS;
+                    p[u] = none;
+                    if (t < b1) {
+                        const float2 ms = part.ms[(size_t)t * part.pitch + n];
+                        p[u] = Stats{ms.x, ms.y, part.dev[(size_t)t * part.pitch + n]};
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < JOIN_UNROLL; ++u) {
+                    const int t = t0 + u * GROUPS;
+                    if (t >= b1) break;
+                    s = join(s, p[u]);
+                    if (TOP) maxima[(t - b0) * ROW + tok] = p[u].m;
+                }
+            }
+        }
+        if (!TOP) continue;
+        __syncthreads();
+        if (my_n < cv.n_c) {
+            for (int t0 = b0 + sub * 64; t0 < b1; t0 += WPT * 64) {
+                const int t = t0 + lane;
+                top.offer(t < b1 ? top_key(maxima[(t - b0) * ROW + my_tok], (uint32_t)t) : 0, o.top_k, lane);
+            }
+        }
+    }
+#pragma unroll
+    for (int off = TOK; off < 64; off <<= 1)
+        s = join(s, Stats{__shfl_xor(s.m, off, 64), __shfl_xor(s.sum, off, 64), __shfl_xor(s.dev, off, 64)});
+    if (lane < TOK) red[wave][lane] = s;
+    __syncthreads();
+    if (tid < TOK) {
+        for (int w = 1; w < JOIN_WAVES; ++w) s = join(s, red[w][tid]);
+        if (TOP) fin[tid] = s;
+        if (n < cv.n_c) {
+            const int64_t gi = cv.n0 + n;
+            if (look_up && a.status != nullptr) report_token(a, gi);
+            write_token(o, gi, s, part.zy ? part.zy[n] : 0.0f);
+        }
+    }
+    if (!TOP) return;
+    __syncthreads();
+    // every wavefront of a token ends with the token's list
+    auto share = [&](TopList& l) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 1; d < WPT; d *= 2) {
+            if (d > 1) __syncthreads();
+            lists[wave][lane] = l.entry;
+            __syncthreads();
+            l.merge(lists[wave ^ d][lane], lane);
+        }
+    };
+    if (WPT > 1) share(top);
+    TopList best;
+    if (my_n < cv.n_c) {
+        const int count = tiles < o.top_k ? tiles : o.top_k;
+        // the k-th largest maximum: k logits are no smaller
+        if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
+        const float* z = Z + (size_t)my_n * ldz;
+        for (int i0 = sub; i0 < count; i0 += WPT * JOIN_UNROLL) {
+            float4 x[JOIN_UNROLL];
+            int v0[JOIN_UNROLL];
+#pragma unroll
+            for (int u = 0; u < JOIN_UNROLL; ++u) {
+                const int i = i0 + u * WPT;
+                v0[u] = i < count && lane * 4 < tile ? (int)top_index(lane_value(top.entry, i < count ? i : 0)) * tile + lane * 4 : a.V;
+                if (v0[u] < a.V) x[u] = *reinterpret_cast<const float4*>(z + v0[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < JOIN_UNROLL; ++u) {
+                const float xx[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) best.offer(v0[u] + q < a.V ? top_key(xx[q], (uint32_t)(v0[u] + q)) : 0, o.top_k, lane);
+            }
+        }
+    }
+    if (WPT > 1) {
+        __syncthreads();
+        share(best);
+    }
+    if (my_n < cv.n_c && sub == 0) write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
 }
 
 // A wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row (16-byte vectors, zero beyond
@@ -261,6 +368,20 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
     if (partial.parts == 1) return;
     if (top) join_parts_kernel<true><<<(unsigned)cv.n_c, 64, 0, st>>>(Z, ldz, a, o, cv, partial);
     else join_parts_kernel<false><<<(unsigned)cv.n_c, 64, 0, st>>>(Z, ldz, a, o, cv, partial);
+}
+
+void launch_stats_join(const StatsPart& part, int32_t tiles, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+                       const StatsOut& o, ChunkView cv, hipStream_t st) {
+    auto go = [&](auto tok) {
+        constexpr int TOK = decltype(tok)::value;
+        const unsigned blocks = (unsigned)ceil_div(cv.n_c, TOK);
+        if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, tiles, tile, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, tiles, tile, Z, ldz, a, look_up, o, cv);
+    };
+    // as many tokens a workgroup as leave every compute unit one
+    if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 1>{});
+    else if (cv.n_c <= 16 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
+    else go(std::integral_constant<int, 16>{});
 }
 
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {

@@ -26,21 +26,64 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
     return ((uint64_t)hi << 32) | lo;
 }
 
+// The value of lane (own lane ^ X): by data-parallel primitives where one says it, else through the LDS crossbar.
+template <int X>
+__device__ __forceinline__ uint32_t xor_lane(uint32_t v) {
+    constexpr int ctrl = X == 1 ? 0xB1 : X == 2 ? 0x4E : X == 3 ? 0x1B : X == 7 ? 0x141 : X == 8 ? 0x128 : X == 15 ? 0x140 : 0;
+    if constexpr (ctrl != 0) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, true);
+    else return (uint32_t)__shfl_xor((int)v, X, 64);
+}
+template <int X>
+__device__ __forceinline__ uint64_t xor_lane(uint64_t v) {
+    return ((uint64_t)xor_lane<X>((uint32_t)(v >> 32)) << 32) | xor_lane<X>((uint32_t)v);
+}
+// Of a pair of lanes X apart, the one with the lower number (bit BIT clear) keeps the larger key.
+template <int X, int BIT>
+__device__ __forceinline__ uint64_t exchange(uint64_t v, int lane) {
+    const uint64_t o = xor_lane<X>(v);
+    return ((lane & BIT) == 0) == (o > v) ? o : v;
+}
+// A sequence that falls and then rises (or is such a one's rotation) in descending order: 2 N lanes, N the first distance.
+template <int N>
+__device__ __forceinline__ uint64_t settle_bitonic(uint64_t v, int lane) {
+    v = exchange<N, N>(v, lane);
+    if constexpr (N > 1) v = settle_bitonic<N / 2>(v, lane);
+    return v;
+}
+// 64 keys in descending order: sorted runs of N are mirrored against each other to runs of 2 N.
+template <int N = 1>
+__device__ __forceinline__ uint64_t sort_lanes(uint64_t v, int lane) {
+    v = exchange<2 * N - 1, N>(v, lane);
+    if constexpr (N > 1) v = settle_bitonic<N / 2>(v, lane);
+    if constexpr (N < 32) v = sort_lanes<2 * N>(v, lane);
+    return v;
+}
+
 struct TopList {
     uint64_t entry = 0;       // this lane's
-    uint64_t least = 0;       // entry k - 1: what a newcomer has to exceed
+    uint64_t least = 0;       // entry k - 1 (or a bound below it that is known from elsewhere): what a newcomer has to exceed
     float floor = -__builtin_inff();   // the same as a logit: a lower one need not be looked at (-infinity while there are not k)
 
-    // All lanes: lane l's key joins the list if it exceeds `least`.
-    __device__ __forceinline__ void offer(uint64_t key, int k) {
+    // All lanes: lane l's key joins the list if it exceeds `least`. Few newcomers are inserted one by one (some 80 cycles each), more
+    // are sorted and merged.
+    __device__ __forceinline__ void offer(uint64_t key, int k, int lane) {
         uint64_t hits = __ballot(key > least);
         if (hits == 0) return;
-        do {
-            const int l = __builtin_ctzll(hits);
-            hits &= hits - 1;
-            insert(lane_value(key, l));
-        } while (hits);
+        if (__builtin_popcountll(hits) > 16) {
+            merge(sort_lanes(key, lane), lane);
+        } else {
+            do {
+                const int l = __builtin_ctzll(hits);
+                hits &= hits - 1;
+                insert(lane_value(key, l));
+            } while (hits);
+        }
         settle(k);
+    }
+    // Joins keys in descending order: the larger of each mirrored pair are the 64 largest, in bitonic order.
+    __device__ __forceinline__ void merge(uint64_t sorted, int lane) {
+        const uint64_t o = xor_lane<63>(sorted);
+        entry = settle_bitonic<32>(entry > o ? entry : o, lane);
     }
     // A sorted insertion: whoever is smaller moves one lane up.
     __device__ __forceinline__ void insert(uint64_t key) {
@@ -51,8 +94,15 @@ struct TopList {
         entry = entry > key ? entry : before > key ? key : before;
     }
     __device__ __forceinline__ void settle(int k) {
-        least = lane_value(entry, k - 1);
+        const uint64_t last = lane_value(entry, k - 1);
+        least = last > least ? last : least;
         floor = (uint32_t)(least >> 32) <= 1u ? -__builtin_inff() : top_value(least);
+    }
+    // Only keys whose value is at least `key`'s will be wanted.
+    __device__ __forceinline__ void at_least(uint64_t key) {
+        if (key == 0) return;
+        least = (key >> 32 << 32) - 1;
+        floor = (uint32_t)(key >> 32) <= 1u ? -__builtin_inff() : top_value(key);
     }
 };
 
