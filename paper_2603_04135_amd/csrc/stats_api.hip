@@ -17,7 +17,7 @@ constexpr size_t LOGITS_CHUNK_BYTES = (size_t)8 << 30;
 struct Regions {                            // offsets into the workspace
     int32_t Vp, n_cp;
     size_t row_bytes;
-    size_t o_hc, o_scale, o_z, o_pstats, o_pkeys, o_ms, o_dev, o_zy;                     // forward
+    size_t o_hc, o_scale, o_z, o_pstats, o_pkeys, o_mx, o_sd, o_zy, o_tau;                    // forward
     size_t o_wt, o_dwpart, o_dwacc, o_hct, o_fpart, o_y, o_rowc;                         // backward
     bool direct_w;
     int f32_parts;
@@ -41,8 +41,9 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
         r.o_z = take(s.dtype == F32 || top_k > 0 ? n * r.Vp * 4 : 0);
         // (128-row tiles have at most 128 tokens: no more pairs than 256-row tiles of 256)
         const size_t pairs = s.dtype == F32 ? 0 : n * mfma_logits_row_tiles(s.V);
-        r.o_ms = take(pairs * sizeof(float2));
-        r.o_dev = take(pairs * 4);
+        r.o_mx = take(pairs * STATS_GROUPS * 4);
+        r.o_sd = take(pairs * sizeof(float2));
+        r.o_tau = take(s.dtype == F32 ? 0 : n * 4);
         r.o_zy = take(s.dtype == F32 ? 0 : n * 4);
         r.o_y = take(s.dtype == F32 ? 0 : n * 4);
         // float32: rows are cut into parts only where there are fewer than 4 per compute unit: at most 8 * DEFAULT_CUS parts in all
@@ -212,17 +213,27 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
             if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
         }
-        StatsTiles t{{reinterpret_cast<float2*>(w + r.o_ms), reinterpret_cast<float*>(w + r.o_dev),
+        StatsTiles t{{reinterpret_cast<float*>(w + r.o_mx), reinterpret_cast<float2*>(w + r.o_sd),
                       logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, few ? cv.n_c : cv.n_cp},
-                     tokens, few ? nullptr : y, cv};
-        {
+                     tokens, few ? nullptr : y, cv, nullptr, 0, -1};
+        auto gemm = [&]() {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
             if (s.dtype == BF16) launch_stats_bf16(g, t, st);
             else launch_stats_i8(g, sc, t, st);
+        };
+        int32_t groups = 0;
+        const int lead = stats_lead_tiles(s.V, cv.n_c, top_k, cus, &groups);
+        if (lead > 0) {
+            float* tau = reinterpret_cast<float*>(w + r.o_tau);
+            t.count = lead;
+            gemm();
+            StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
+            launch_stats_bound(t.part, groups, top_k, cv, tau, st);
+            t.tau = tau; t.first = lead; t.count = -1;
         }
+        gemm();
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        const int32_t tile = logits_tile_rows(cv.n_c);
-        launch_stats_join(t.part, (int32_t)ceil_div(s.V, tile), tile, Z, r.Vp, tokens, few, out, cv, st);
+        launch_stats_join(t.part, logits_tile_rows(cv.n_c), Z, r.Vp, tokens, few, out, cv, st);
     }
     return check_launch("dppo_token_stats");
 }

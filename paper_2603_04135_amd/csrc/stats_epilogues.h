@@ -95,16 +95,17 @@ struct EpiOut : OperandTag<I8> {
     static constexpr bool SWAP = false;
 };
 
-// Softmax statistics of every token over the tile's vocabulary rows, {max, sum exp(z - max)} and sum (z - max) exp(z - max) (see
-// Stats), in registers and combined across the wavefronts through LDS; the target's logit from the accumulator that holds it; with
-// STORE the logits themselves, row-major by token, for the top alternatives.
+// Softmax statistics of every token over the tile's vocabulary rows (see Stats and StatsPart), in registers and combined across the
+// wavefronts through LDS; the target's logit from the accumulator that holds it; with STORE the logits that may be among the top
+// alternatives, row-major by token. A group (the rows of one wavefront) is stored for the tokens whose bound tau its maximum exceeds:
+// top_k groups of lower vocabulary entries reach tau, so nothing else can be among the alternatives (an equal logit loses to theirs).
 template <bool I8, bool STORE>
 struct EpiStats : OperandTag<I8> {
     StatsPart part;
     OperandScales scales;
     // y[n]: targets looked up before, or NULL: from tokens.ids (NULL: no targets)
     TokenArgs tokens; const int32_t* y; int64_t n0; int n_c;
-    float* Z; int64_t ldz;
+    float* Z; int64_t ldz; const float* tau;
 
     __device__ __forceinline__ void look_up(int, int) const {}
     template <class Cfg, class Acc>
@@ -113,17 +114,8 @@ struct EpiStats : OperandTag<I8> {
         const float NEG_INF = -__builtin_inff();
         f32x4 z[MI][NI];
         to_logits<Cfg>(acc, z, c, scales);
-        if (STORE) {
-            // whole tiles, the padding of the vocabulary too (the pitch holds it)
-#pragma unroll
-            for (int ni = 0; ni < NI; ++ni) {
-                const int n = c.n0 + ni * MB + acc_col(c.lane);
-                if (n >= n_c) continue;
-                float* dst = Z + (size_t)n * ldz + c.m0 + acc_row(c.lane, 0);
-#pragma unroll
-                for (int mi = 0; mi < MI; ++mi) *reinterpret_cast<f32x4*>(dst + mi * MB) = z[mi][ni];
-            }
-        }
+        static_assert(Cfg::WGM == STATS_GROUPS, "a wavefront's rows = a group");
+        float* mx_out = part.mx + (size_t)(c.tm * STATS_GROUPS + c.wave_m) * part.pitch;
         float3* red = reinterpret_cast<float3*>(c.smem);
         auto reduce = [&](auto full_tag) __attribute__((always_inline)) {
             constexpr bool FULL = decltype(full_tag)::value;
@@ -139,6 +131,16 @@ struct EpiStats : OperandTag<I8> {
                     }
                 m = fmaxf(m, __shfl_xor(m, 16, 64));
                 m = fmaxf(m, __shfl_xor(m, 32, 64));
+                const int n = c.n0 + ni * MB + acc_col(c.lane);
+                if (n < n_c) {
+                    if (c.lane < MB) mx_out[n] = m;
+                    // whole groups, the padding of the vocabulary too (the pitch holds it)
+                    if (STORE && (!tau || m > tau[n])) {
+                        float* dst = Z + (size_t)n * ldz + c.m0 + acc_row(c.lane, 0);
+#pragma unroll
+                        for (int mi = 0; mi < MI; ++mi) *reinterpret_cast<f32x4*>(dst + mi * MB) = z[mi][ni];
+                    }
+                }
                 const float ref = m == NEG_INF ? 0.0f : m;
                 float sum = 0.0f, dev = 0.0f;
 #pragma unroll
@@ -192,8 +194,7 @@ struct EpiStats : OperandTag<I8> {
                 s = join(s, Stats{r.x, r.y, r.z});
             }
             const size_t at = (size_t)c.tm * part.pitch + n;
-            part.ms[at] = make_float2(s.m, s.sum);
-            part.dev[at] = s.dev;
+            part.sd[at] = make_float2(s.sum, s.dev);
         }
     }
 
@@ -272,14 +273,14 @@ namespace {
 // The tile of the vocabulary GEMM by the number of tokens, as for the log-probabilities alone (see CfgFew): up to 192 tokens
 // columns that read the tokens' rows of H where they lie, through the map. Beyond, the rows are contiguous.
 template <class Epi>
-void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st) {
+void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st, int first = 0, int count = -1) {
     auto mapped = [&](auto cfg) {
-        launch<decltype(cfg), A_ROWS, WG_ROUNDS, B_MAP>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, 0, -1, 1, -1, (int)g.h_rows, 0, g.map, 0);
+        launch<decltype(cfg), A_ROWS, WG_ROUNDS, B_MAP>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count, 1, -1, (int)g.h_rows, 0, g.map, 0);
     };
     if (g.n <= 96) mapped(CfgFew<96>{});
     else if (g.n <= 128) mapped(CfgFew<128>{});
     else if (g.n <= STATS_MAP_TOKENS) mapped(CfgBig192{});
-    else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st);
+    else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count);
 }
 template <class Epi>
 hipError_t allow_logits() {
@@ -293,8 +294,8 @@ template <bool I8>
 void launch_stats_tiles(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st) {
     auto go = [&](auto e) {
         e.part = t.part; e.scales = s; e.tokens = t.tokens; e.y = t.y; e.n0 = t.cv.n0; e.n_c = t.cv.n_c;
-        e.Z = reinterpret_cast<float*>(g.C); e.ldz = g.ldc;
-        launch_logits(g, e, st);
+        e.Z = reinterpret_cast<float*>(g.C); e.ldz = g.ldc; e.tau = t.tau;
+        launch_logits(g, e, st, t.first, t.count);
     };
     if (g.C) go(EpiStats<I8, true>{});
     else go(EpiStats<I8, false>{});

@@ -30,11 +30,15 @@ struct PartialStats {
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
 
-// Per-tile statistics of the vocabulary GEMM: {max, sum} and dev of row tile t and token n at [t * pitch + n]; zy[n]: target logits (or NULL).
-struct StatsPart { float2* ms; float* dev; float* zy; int32_t pitch; };
-// Joins a token's tiles (tile: rows of one) and picks the top alternatives from the stored logits of the tiles that can hold them.
-void launch_stats_join(const StatsPart& part, int32_t tiles, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows: mx[g * pitch + n] is group g's maximum for token n,
+// sd[t * pitch + n] = {sum, dev} of tile t against its own maximum; zy[n]: target logits (or NULL).
+constexpr int STATS_GROUPS = 2;
+struct StatsPart { float* mx; float2* sd; float* zy; int32_t pitch; };
+// Joins a token's tiles (tile: rows of one) and picks the top alternatives from the stored logits of the groups that can hold them.
+void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st);
+// tau[n] = the top_k-th largest maximum of token n's first `groups` groups (at least top_k).
+void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, ChunkView cv, float* tau, hipStream_t st);
 
 // Copies of the tokens' rows (row_bytes: a multiple of 4; below 16-byte alignment they are taken for float32), their targets (-1 without ids), clamped rows and scales;
 // any of the outputs may be NULL.
@@ -87,7 +91,12 @@ constexpr int32_t STATS_MAP_TOKENS = 192;
 // Vocabulary rows of a tile for n tokens.
 inline int32_t logits_tile_rows(int32_t n) { return n <= 128 ? 128 : 256; }
 // The same GEMM with the statistics in its epilogue (C NULL: the logits are not stored; otherwise ldc holds whole tiles).
-struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkView cv; };
+// tau: of groups whose maximum does not exceed tau[n] the logits are not stored (NULL: all are). first, count: tiles of the launch in the
+// order of the walk (count < 0: to the last).
+struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkView cv; const float* tau; int first, count; };
+// Leading tiles of the walk, whole bands of rows from vocabulary entry 0 on, that a call with alternatives launches ahead of the rest
+// (0: none), and how many groups of rows they are.
+int stats_lead_tiles(int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups);
 int mfma_stats_setup(int* compute_units);
 int mfma_i8_setup(int* compute_units);
 void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, hipStream_t st);

@@ -161,17 +161,19 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
 }
 
 // Joins the per-tile statistics of TOK tokens per workgroup, and picks their top alternatives. The k largest logits of a token lie in
-// the k tiles with the largest maxima (in the order of maximum, then tile: every tile ahead of another one holds a logit that is ahead
-// of all of the other's), so that of the stored logits only those tiles are read: k KB of a row of V.
+// the k groups with the largest maxima (in the order of maximum, then group: every group ahead of another one holds a logit that is
+// ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
 // The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
-// list the tiles and their logits.
+// list the groups and their logits.
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 4;
 template <int TOK, bool TOP>
-__global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tiles, int32_t tile, const float* __restrict__ Z,
+__global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tile, const float* __restrict__ Z,
                                                                   int64_t ldz, TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
     constexpr int GROUPS = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;      // lane groups of the tiles; wavefronts per token
-    constexpr int ROW = TOK == 1 ? 1 : TOK + 1, BLOCK = JOIN_MAXIMA / TOK;  // maxima in LDS: tiles of a block, their row pitch
-    __shared__ float maxima[TOP ? BLOCK * ROW : 1];
+    constexpr int ROW = TOK + 1;                                            // maxima in LDS: row pitch, tiles of a block
+    constexpr int BLOCK = JOIN_MAXIMA / TOK / STATS_GROUPS;
+    static_assert(STATS_GROUPS == 2, "maxima of a tile");
+    __shared__ float maxima[TOP ? STATS_GROUPS * BLOCK * ROW : 1];
     __shared__ Stats red[JOIN_WAVES][TOK];
     __shared__ Stats fin[TOK];
     __shared__ uint64_t lists[TOP && WPT > 1 ? JOIN_WAVES : 1][TOP_MAX];
@@ -179,6 +181,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
     const int tok = tid % TOK, group = tid / TOK, n = blockIdx.x * TOK + tok;
     const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
     const Stats none = no_stats();
+    const int tiles = (a.V + tile - 1) / tile, rows = tile / STATS_GROUPS, groups = (a.V + rows - 1) / rows;
     Stats s = none;
     TopList top;
     for (int b0 = 0; b0 < tiles; b0 += BLOCK) {
@@ -186,31 +189,41 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
         if (TOP && b0 > 0) __syncthreads();
         if (n < cv.n_c) {
             for (int t0 = b0 + group; t0 < b1; t0 += GROUPS * JOIN_UNROLL) {
-                Stats p[JOIN_UNROLL];
+                float2 sd[JOIN_UNROLL];
+                float m0[JOIN_UNROLL], m1[JOIN_UNROLL];
 #pragma unroll
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
                     const int t = t0 + u * GROUPS;
-                    p[u] = none;
-                    if (t < b1) {
-                        const float2 ms = part.ms[(size_t)t * part.pitch + n];
-                        p[u] = Stats{ms.x, ms.y, part.dev[(size_t)t * part.pitch + n]};
-                    }
+                    if (t >= b1) break;
+                    m0[u] = part.mx[(size_t)(2 * t) * part.pitch + n];
+                    m1[u] = part.mx[(size_t)(2 * t + 1) * part.pitch + n];
+                    sd[u] = part.sd[(size_t)t * part.pitch + n];
                 }
 #pragma unroll
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
                     const int t = t0 + u * GROUPS;
                     if (t >= b1) break;
-                    s = join(s, p[u]);
-                    if (TOP) maxima[(t - b0) * ROW + tok] = p[u].m;
+                    s = join(s, Stats{fmaxf(m0[u], m1[u]), sd[u].x, sd[u].y});
+                    if (TOP) {
+                        maxima[(2 * (t - b0)) * ROW + tok] = m0[u];
+                        maxima[(2 * (t - b0) + 1) * ROW + tok] = m1[u];
+                    }
                 }
             }
         }
         if (!TOP) continue;
         __syncthreads();
         if (my_n < cv.n_c) {
-            for (int t0 = b0 + sub * 64; t0 < b1; t0 += WPT * 64) {
-                const int t = t0 + lane;
-                top.offer(t < b1 ? top_key(maxima[(t - b0) * ROW + my_tok], (uint32_t)t) : 0, o.top_k, lane);
+            const int g1 = 2 * b1 < groups ? 2 * b1 : groups;
+            if (b0 == 0 && g1 > 128) {
+                // the lanes' own maxima bound what is listed: a quarter more than k instead of k (1 + log(groups / k))
+                float m = -__builtin_inff();
+                for (int g = sub * 64 + lane; g < g1; g += WPT * 64) m = fmaxf(m, maxima[g * ROW + my_tok]);
+                top.at_least(kth_of_lanes(m, o.top_k, lane));
+            }
+            for (int g0 = 2 * b0 + sub * 64; g0 < g1; g0 += WPT * 64) {
+                const int g = g0 + lane;
+                top.offer(g < g1 ? top_key(maxima[(g - 2 * b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
             }
         }
     }
@@ -243,17 +256,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
     if (WPT > 1) share(top);
     TopList best;
     if (my_n < cv.n_c) {
-        const int count = tiles < o.top_k ? tiles : o.top_k;
+        const int count = groups < o.top_k ? groups : o.top_k;
         // the k-th largest maximum: k logits are no smaller
         if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
         const float* z = Z + (size_t)my_n * ldz;
-        for (int i0 = sub; i0 < count; i0 += WPT * JOIN_UNROLL) {
+        // rows / 4 lanes read a group
+        const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
+        for (int i0 = sub * per; i0 < count; i0 += WPT * per * JOIN_UNROLL) {
             float4 x[JOIN_UNROLL];
             int v0[JOIN_UNROLL];
 #pragma unroll
             for (int u = 0; u < JOIN_UNROLL; ++u) {
-                const int i = i0 + u * WPT;
-                v0[u] = i < count && lane * 4 < tile ? (int)top_index(lane_value(top.entry, i < count ? i : 0)) * tile + lane * 4 : a.V;
+                const int i = i0 + u * WPT * per + which;
+                const uint32_t g = ~(uint32_t)__shfl((int)(uint32_t)top.entry, i < count ? i : 0, 64);
+                v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
                 if (v0[u] < a.V) x[u] = *reinterpret_cast<const float4*>(z + v0[u]);
             }
 #pragma unroll
@@ -269,6 +285,26 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
         share(best);
     }
     if (my_n < cv.n_c && sub == 0) write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
+}
+
+// tau[n]: one wavefront per token lists the maxima of the leading groups, read with neighbouring tokens side by side.
+constexpr int BOUND_TOK = 16, BOUND_BLOCK = 640;
+__global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32_t groups, int32_t top_k, int32_t n_c, float* __restrict__ tau) {
+    __shared__ float maxima[BOUND_BLOCK * (BOUND_TOK + 1)];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tok = tid % BOUND_TOK, n = blockIdx.x * BOUND_TOK + tok, my_n = blockIdx.x * BOUND_TOK + wave;
+    TopList top;
+    for (int g0 = 0; g0 < groups; g0 += BOUND_BLOCK) {
+        const int g1 = groups - g0 < BOUND_BLOCK ? groups : g0 + BOUND_BLOCK;
+        if (g0 > 0) __syncthreads();
+        if (n < n_c) {
+            for (int g = g0 + tid / BOUND_TOK; g < g1; g += 1024 / BOUND_TOK) maxima[(g - g0) * (BOUND_TOK + 1) + tok] = part.mx[(size_t)g * part.pitch + n];
+        }
+        __syncthreads();
+        for (int i = g0; i < g1; i += 64)
+            top.offer(i + lane < g1 && my_n < n_c ? top_key(maxima[(i + lane - g0) * (BOUND_TOK + 1) + wave], (uint32_t)(i + lane)) : 0, top_k, lane);
+    }
+    if (lane == 0 && my_n < n_c) tau[my_n] = top_value(lane_value(top.entry, top_k - 1));
 }
 
 // A wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row (16-byte vectors, zero beyond
@@ -370,18 +406,23 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
     else join_parts_kernel<false><<<(unsigned)cv.n_c, 64, 0, st>>>(Z, ldz, a, o, cv, partial);
 }
 
-void launch_stats_join(const StatsPart& part, int32_t tiles, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st) {
     auto go = [&](auto tok) {
         constexpr int TOK = decltype(tok)::value;
         const unsigned blocks = (unsigned)ceil_div(cv.n_c, TOK);
-        if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, tiles, tile, Z, ldz, a, look_up, o, cv);
-        else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, tiles, tile, Z, ldz, a, look_up, o, cv);
+        if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
     };
-    // as many tokens a workgroup as leave every compute unit one
-    if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 1>{});
-    else if (cv.n_c <= 16 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
+    // As many tokens a workgroup as leave every compute unit at most one, from 4 on. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens
+    // 25.6 / 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83; one token 15.5 / 19.6 / 28.4 (1 token a workgroup 17.7).
+    if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
+    else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 16>{});
+}
+
+void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, ChunkView cv, float* tau, hipStream_t st) {
+    stats_bound_kernel<<<(unsigned)ceil_div(cv.n_c, BOUND_TOK), 1024, 0, st>>>(part, groups, top_k, cv.n_c, tau);
 }
 
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {

@@ -59,6 +59,11 @@ __device__ __forceinline__ uint64_t sort_lanes(uint64_t v, int lane) {
     return v;
 }
 
+// The k-th largest of the lanes' logits (NaN: the lane has none): a bound that k logits reach.
+__device__ __forceinline__ uint64_t kth_of_lanes(float z, int k, int lane) {
+    return lane_value(sort_lanes(top_key(z, 0) >> 32, lane), k - 1) << 32;
+}
+
 struct TopList {
     uint64_t entry = 0;       // this lane's
     uint64_t least = 0;       // entry k - 1 (or a bound below it that is known from elsewhere): what a newcomer has to exceed
@@ -98,9 +103,9 @@ struct TopList {
         least = last > least ? last : least;
         floor = (uint32_t)(least >> 32) <= 1u ? -__builtin_inff() : top_value(least);
     }
-    // Only keys whose value is at least `key`'s will be wanted.
+    // Only keys whose value is at least `key`'s will be wanted: k of those on offer reach it.
     __device__ __forceinline__ void at_least(uint64_t key) {
-        if (key == 0) return;
+        if ((uint32_t)(key >> 32) <= 1u) return;
         least = (key >> 32 << 32) - 1;
         floor = (uint32_t)(key >> 32) <= 1u ? -__builtin_inff() : top_value(key);
     }

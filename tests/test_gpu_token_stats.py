@@ -108,6 +108,7 @@ def check_stats(out, z, y, k, z_err=0.0):
     ("bf16", 1, 64, 1, 1), ("bf16", 1, 128, 20011, 20), ("bf16", 2, 64, 257, 64), ("bf16", 95, 64, 700, 3), ("bf16", 97, 128, 256, 8),
     ("bf16", 128, 192, 1000, 0), ("bf16", 129, 64, 513, 20), ("bf16", 192, 256, 4099, 5), ("bf16", 193, 64, 300, 1),
     ("bf16", 256, 64, 64, 64), ("bf16", 257, 128, 20011, 20), ("bf16", 700, 512, 2049, 33), ("bf16", 520, 64, 33333, 64),
+    ("bf16", 300, 64, 70001, 20), ("bf16", 300, 128, 20011, 3), ("bf16", 1500, 64, 16700, 1), ("i8", 300, 128, 70001, 20),
     ("i8", 1, 128, 1, 1), ("i8", 1, 128, 20011, 20), ("i8", 50, 256, 1000, 7), ("i8", 100, 128, 300, 0), ("i8", 150, 384, 513, 64),
     ("i8", 192, 128, 4099, 2), ("i8", 193, 128, 255, 20), ("i8", 513, 256, 20011, 20), ("i8", 300, 1152, 257, 9)])
 @pytest.mark.parametrize("positions", ["loss_pos", "identity", "no targets"])
@@ -137,8 +138,9 @@ def test_statistics_of_ordinary_values(P, dtype, N, V):
 
 @pytest.mark.parametrize("dtype,N", [("f32", 5), ("f32", 300), ("bf16", 5), ("bf16", 150), ("bf16", 600), ("i8", 5), ("i8", 600)])
 @pytest.mark.parametrize("kind", ["all equal", "two values", "ascending", "descending", "copies"])
-def test_equal_logits_go_by_id(P, dtype, N, kind):
-    D, V, k = 128, 9001, 64
+@pytest.mark.parametrize("k", [64, 3])
+def test_equal_logits_go_by_id(P, dtype, N, kind, k):
+    D, V = 128, 9001
     c = Case(dtype, N, D, V, seed=3)
     i = torch.arange(V, device=DEV)
     c.H.zero_()
@@ -168,17 +170,18 @@ def test_equal_logits_go_by_id(P, dtype, N, kind):
 
 @pytest.mark.parametrize("dtype,N", [("f32", 3), ("f32", 300), ("bf16", 3), ("bf16", 150), ("bf16", 600)])
 @pytest.mark.parametrize("kind", ["tile", "most", "lowest", "lowest all", "all", "nan", "inf"])
-def test_masked_and_non_finite_logits(P, dtype, N, kind):
+@pytest.mark.parametrize("V,k", [(5001, 20), (9001, 3)])
+def test_masked_and_non_finite_logits(P, dtype, N, kind, V, k):
     """Column 0 of W is added to the logits. -infinity and the type's lowest value carry no weight and come last; a NaN or
     +infinity makes the row's statistics NaN and leaves distinct alternatives in range."""
-    D, V, k = 64, 5001, 20
+    D = 64
     c = Case(dtype, N, D, V, seed=6)
     c.H[:, 0] = 1
     low = float(torch.finfo(DTYPES[dtype]).min)
     if kind == "tile":
         c.W[256:512, 0] = -np.inf
     elif kind == "most":
-        c.W[7:, 0] = -np.inf                     # fewer finite entries than alternatives
+        c.W[k // 3:, 0] = -np.inf                # fewer finite entries than alternatives
     elif kind == "lowest":
         c.W[:4000, 0] = low
     elif kind == "lowest all":
