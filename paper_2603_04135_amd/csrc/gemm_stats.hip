@@ -1,5 +1,5 @@
 // bfloat16 GEMMs of the token statistics and their gradient.
-#include "stats_epilogues.h"
+#include "few_tokens.h"
 
 namespace dppo {
 namespace {
@@ -14,6 +14,7 @@ typedef EpiStore<2> EpiStoreDW16;
 hipError_t allow_all() {
     hipError_t e = allow_logits<EpiStats<false, false>>();
     if (e == hipSuccess) e = allow_logits<EpiStats<false, true>>();
+    if (e == hipSuccess) e = allow_few<false, FewStats<false>>();
     if (e == hipSuccess) e = allow_lds<CfgBig, EpiStatsGrad>();
     if (e == hipSuccess) e = allow_lds<CfgGrad, EpiStoreDW16, A_BLK_KM, WG_RANGES, B_BLK>();
     return e;
@@ -23,8 +24,8 @@ hipError_t allow_all() {
 
 int mfma_stats_setup(int* compute_units) { return g_setup.run(&allow_all, compute_units); }
 
-void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, hipStream_t st) {
-    launch_stats_tiles<false>(g, OperandScales{nullptr, nullptr, nullptr, 0}, t, st);
+void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, int cus, hipStream_t st) {
+    launch_stats_tiles<false>(g, OperandScales{nullptr, nullptr, nullptr, 0}, t, cus, st);
 }
 
 int stats_lead_tiles(int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups) {

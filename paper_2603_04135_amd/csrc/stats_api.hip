@@ -39,7 +39,7 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
         r.o_hc = take(s.dtype == F32 ? 0 : n * r.row_bytes);
         r.o_scale = take(s.dtype == I8 ? n * 4 : 0);
         r.o_z = take(s.dtype == F32 || top_k > 0 ? n * r.Vp * 4 : 0);
-        // (128-row tiles have at most 128 tokens: no more pairs than 256-row tiles of 256)
+        // (at most 128 tokens in 128-row tiles, 16 in 32-row ones: no more pairs than 256 tokens in 256-row tiles)
         const size_t pairs = s.dtype == F32 ? 0 : n * mfma_logits_row_tiles(s.V);
         r.o_mx = take(pairs * STATS_GROUPS * 4);
         r.o_sd = take(pairs * sizeof(float2));
@@ -218,8 +218,8 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
                      tokens, few ? nullptr : y, cv, nullptr, 0, -1};
         auto gemm = [&]() {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
-            if (s.dtype == BF16) launch_stats_bf16(g, t, st);
-            else launch_stats_i8(g, sc, t, st);
+            if (s.dtype == BF16) launch_stats_bf16(g, t, cus, st);
+            else launch_stats_i8(g, sc, t, cus, st);
         };
         int32_t groups = 0;
         const int lead = stats_lead_tiles(s.V, cv.n_c, top_k, cus, &groups);
@@ -233,7 +233,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         }
         gemm();
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        launch_stats_join(t.part, logits_tile_rows(cv.n_c), Z, r.Vp, tokens, few, out, cv, st);
+        launch_stats_join(t.part, logits_tile_rows(cv.n_c, g.k2, s.dtype == I8), Z, r.Vp, tokens, few, out, cv, st);
     }
     return check_launch("dppo_token_stats");
 }
@@ -358,7 +358,8 @@ int dppo_matmul_i8(int64_t T, int32_t V, int32_t D, const int8_t* X, const float
     if (T == 0) return DPPO_OK;
     if (!X || !x_scale || !W || !w_scale || !Y) return fail(DPPO_ERR_INVALID_ARG, "a required array pointer is NULL");
     if (!aligned16(X) || !aligned16(W)) return fail(DPPO_ERR_INVALID_ARG, "X and W must be 16-byte aligned");
-    if ((rc = mfma_i8_setup(nullptr)) != DPPO_OK) return rc;
+    int cus = 0;
+    if ((rc = mfma_i8_setup(&cus)) != DPPO_OK) return rc;
     hipStream_t st = (hipStream_t)stream;
     StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
     constexpr int64_t CHUNK = 32768;
@@ -366,7 +367,7 @@ int dppo_matmul_i8(int64_t T, int32_t V, int32_t D, const int8_t* X, const float
         const int32_t n = (int32_t)(T - n0 < CHUNK ? T - n0 : CHUNK);
         LogitsOut g{W, V, D / 2, X + (size_t)n0 * D, n, nullptr, n,
                     reinterpret_cast<char*>(Y) + (size_t)n0 * V * element_bytes(out_dtype), V};
-        launch_logits_i8(g, OperandScales{w_scale, x_scale + n0, nullptr, n}, out_dtype == BF16, st);
+        launch_logits_i8(g, OperandScales{w_scale, x_scale + n0, nullptr, n}, out_dtype == BF16, cus, st);
     }
     return check_launch("dppo_matmul_i8");
 }

@@ -40,6 +40,25 @@ __device__ __forceinline__ void to_logits(Acc (&acc)[Cfg::MI][Cfg::NI], f32x4 (&
     }
 }
 
+// Four neighbouring logits of a token: one aligned store, or the first `left` of them one by one.
+template <class Out>
+__device__ __forceinline__ void store_logits(Out* dst, const f32x4& v, bool whole, int left) {
+    if constexpr (sizeof(Out) == 4) {
+        if (whole) { *reinterpret_cast<f32x4*>(dst) = v; return; }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) dst[j] = v[j];
+    } else {
+        const __bf16 b0 = (__bf16)v[0], b1 = (__bf16)v[1], b2 = (__bf16)v[2], b3 = (__bf16)v[3];
+        const uint16_t h[4] = {__builtin_bit_cast(uint16_t, b0), __builtin_bit_cast(uint16_t, b1), __builtin_bit_cast(uint16_t, b2),
+                               __builtin_bit_cast(uint16_t, b3)};
+        if (whole) { *reinterpret_cast<uint2*>(dst) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16); return; }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < left) dst[j] = h[j];
+    }
+}
+
 // Stores the logits, row-major by token: C[n, v]. A lane's four accumulators are four neighbouring vocabulary entries of one token,
 // one store where the pitch allows it.
 template <bool I8, class Out>
@@ -60,30 +79,8 @@ struct EpiOut : OperandTag<I8> {
                 if (!FULL && n >= c.N) continue;
                 Out* dst = C + (size_t)n * ldc + c.m0 + acc_row(c.lane, 0);
 #pragma unroll
-                for (int mi = 0; mi < Cfg::MI; ++mi) {
-                    const f32x4 v = z[mi][ni];
-                    if (FULL) {
-                        if constexpr (sizeof(Out) == 4) {
-                            *reinterpret_cast<f32x4*>(dst + mi * MB) = v;
-                        } else {
-                            const __bf16 b0 = (__bf16)v[0], b1 = (__bf16)v[1], b2 = (__bf16)v[2], b3 = (__bf16)v[3];
-                            const uint32_t lo = (uint32_t)__builtin_bit_cast(uint16_t, b0) | ((uint32_t)__builtin_bit_cast(uint16_t, b1) << 16);
-                            const uint32_t hi = (uint32_t)__builtin_bit_cast(uint16_t, b2) | ((uint32_t)__builtin_bit_cast(uint16_t, b3) << 16);
-                            *reinterpret_cast<uint2*>(dst + mi * MB) = make_uint2(lo, hi);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if (c.m0 + mi * MB + acc_row(c.lane, j) >= c.M) continue;
-                            if constexpr (sizeof(Out) == 4) {
-                                dst[mi * MB + j] = v[j];
-                            } else {
-                                const __bf16 b = (__bf16)v[j];
-                                dst[mi * MB + j] = __builtin_bit_cast(uint16_t, b);
-                            }
-                        }
-                    }
-                }
+                for (int mi = 0; mi < Cfg::MI; ++mi)
+                    store_logits(dst + mi * MB, z[mi][ni], FULL, c.M - (c.m0 + mi * MB + acc_row(c.lane, 0)));
             }
         };
         if (vec && c.bm0 + Cfg::BM <= c.M && c.bn0 + Cfg::BN <= c.N) store(std::true_type{});
@@ -147,7 +144,7 @@ struct EpiStats : OperandTag<I8> {
                 for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const float d = z[mi][ni][j] - ref, e = __builtin_amdgcn_exp2f(d * LOG2E);
+                        const float d = z[mi][ni][j] - ref, e = exp_fast(d);
                         sum += e;
                         dev = fmaf(fmaxf(d, DEV_MIN), e, dev);
                     }
@@ -232,7 +229,7 @@ struct EpiStatsGrad {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const float lp = acc[mi][ni][q] - t.lse;
-                        float g = grad_entry(t, lp, __builtin_amdgcn_exp2f(lp * LOG2E), false);
+                        float g = grad_entry(t, lp, exp_fast(lp), false);
                         // (a padding token's row of zeros times a weight of -infinity is NaN, which dW would sum)
                         g = n < n_c && (FULL || c.bm0 + vloc + q < V) ? g : 0.0f;
                         const __bf16 b = (__bf16)g;   // scalar copy: reading h[q] back right after writing it miscompiles
@@ -247,7 +244,7 @@ struct EpiStatsGrad {
                     for (int q = 0; q < 4; ++q) {
                         if (at != mi * MB + acc_row(c.lane, q)) continue;
                         const float lp = acc[mi][ni][q] - t.lse;
-                        const __bf16 b = (__bf16)grad_entry(t, lp, __builtin_amdgcn_exp2f(lp * LOG2E), true);
+                        const __bf16 b = (__bf16)grad_entry(t, lp, exp_fast(lp), true);
                         *reinterpret_cast<__bf16*>(c.smem + tok * ZPITCH + (c.wave_m * Cfg::WTM + at) * 2) = b;
                     }
             }
@@ -288,25 +285,6 @@ hipError_t allow_logits() {
     if (e == hipSuccess) e = allow_lds<CfgFew<128>, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
     if (e == hipSuccess) e = allow_lds<CfgBig192, Epi, A_ROWS, WG_ROUNDS, B_MAP>();
     if (e == hipSuccess) e = allow_lds<CfgBig, Epi>();
-    return e;
-}
-template <bool I8>
-void launch_stats_tiles(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st) {
-    auto go = [&](auto e) {
-        e.part = t.part; e.scales = s; e.tokens = t.tokens; e.y = t.y; e.n0 = t.cv.n0; e.n_c = t.cv.n_c;
-        e.Z = reinterpret_cast<float*>(g.C); e.ldz = g.ldc; e.tau = t.tau;
-        launch_logits(g, e, st, t.first, t.count);
-    };
-    if (g.C) go(EpiStats<I8, true>{});
-    else go(EpiStats<I8, false>{});
-}
-template <bool I8, class Out>
-EpiOut<I8, Out> out_epilogue(const LogitsOut& g, const OperandScales& s) {
-    EpiOut<I8, Out> e;
-    e.C = reinterpret_cast<Out*>(g.C);
-    e.ldc = g.ldc;
-    e.vec = g.ldc % 4 == 0 && reinterpret_cast<uintptr_t>(g.C) % (4 * sizeof(Out)) == 0;
-    e.scales = s;
     return e;
 }
 }  // namespace

@@ -15,10 +15,13 @@ struct Stats { float m, sum, dev; };
 // exp() is 0 in 32 bits below -104: differences are cut at -150 where they are multiplied by it, so that a logit at -infinity (or
 // at the type's lowest value, whose difference overflows) adds 0 and not 0 * infinity.
 constexpr float DEV_MIN = -150.0f;
+// exp by the hardware's 2^x: one rounding of the argument (relative error 2 d half steps at exp(-d), whose share of a sum is e^-d) and
+// one unit of its own.
+__device__ __forceinline__ float exp_fast(float d) { return __builtin_amdgcn_exp2f(d * 1.4426950408889634f); }
 __device__ __forceinline__ Stats no_stats() { return Stats{-__builtin_inff(), 0.0f, 0.0f}; }
 __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
     const float m = fmaxf(a.m, b.m), ref = m == -__builtin_inff() ? 0.0f : m;
-    const float da = a.m - ref, db = b.m - ref, ea = expf(da), eb = expf(db);
+    const float da = a.m - ref, db = b.m - ref, ea = exp_fast(da), eb = exp_fast(db);
     return Stats{m, a.sum * ea + b.sum * eb,
                  ea * (a.dev + fmaxf(da, DEV_MIN) * a.sum) + eb * (b.dev + fmaxf(db, DEV_MIN) * b.sum)};
 }
@@ -30,7 +33,7 @@ struct PartialStats {
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
 
-// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows: mx[g * pitch + n] is group g's maximum for token n,
+// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows (logits_tile_groups; a unit of the kernel for few tokens is one): mx[g * pitch + n] is group g's maximum for token n,
 // sd[t * pitch + n] = {sum, dev} of tile t against its own maximum; zy[n]: target logits (or NULL).
 constexpr int STATS_GROUPS = 2;
 struct StatsPart { float* mx; float2* sd; float* zy; int32_t pitch; };
@@ -88,8 +91,12 @@ struct LogitsOut {
     void* C; int64_t ldc;
 };
 constexpr int32_t STATS_MAP_TOKENS = 192;
-// Vocabulary rows of a tile for n tokens.
-inline int32_t logits_tile_rows(int32_t n) { return n <= 128 ? 128 : 256; }
+// Vocabulary rows of a tile for n tokens with operand rows of 2 k2 bytes, and the groups of rows that it is cut into: up to 16 tokens a
+// kernel of their own, with operand rows of up to 8 KB (8-bit operands 6 KB), which is what its registers hold.
+constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 = 8192, FEW_ROW_BYTES_I8 = 6144;
+inline bool few_tokens(int32_t n, int32_t k2, bool i8) { return n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16); }
+inline int32_t logits_tile_rows(int32_t n, int32_t k2, bool i8) { return few_tokens(n, k2, i8) ? FEW_TILE_ROWS : n <= 128 ? 128 : 256; }
+inline int32_t logits_tile_groups(int32_t tile) { return tile == FEW_TILE_ROWS ? 1 : STATS_GROUPS; }
 // The same GEMM with the statistics in its epilogue (C NULL: the logits are not stored; otherwise ldc holds whole tiles).
 // tau: of groups whose maximum does not exceed tau[n] the logits are not stored (NULL: all are). first, count: tiles of the launch in the
 // order of the walk (count < 0: to the last).
@@ -99,9 +106,9 @@ struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkVie
 int stats_lead_tiles(int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups);
 int mfma_stats_setup(int* compute_units);
 int mfma_i8_setup(int* compute_units);
-void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, hipStream_t st);
-void launch_stats_i8(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, hipStream_t st);
-void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, hipStream_t st);  // C float32 or bfloat16
+void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, int cus, hipStream_t st);
+void launch_stats_i8(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, int cus, hipStream_t st);
+void launch_logits_i8(const LogitsOut& g, const OperandScales& s, bool out_bf16, int cus, hipStream_t st);  // C float32 or bfloat16
 // bfloat16 gradient entries of a chunk in the blocked layout (see launch_mfma_logits_grad).
 void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc, ChunkView cv, const int32_t* y, const StatsGrad& g, void* G,
                             int32_t Vp, hipStream_t st);

@@ -86,7 +86,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
         for (int u = 0; u < ROWS_UNROLL; ++u)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const float d = x[u][q] - ref, e = expf(d);
+                const float d = x[u][q] - ref, e = exp_fast(d);
                 b.sum += e;
                 b.dev = fmaf(fmaxf(d, DEV_MIN), e, b.dev);
             }
@@ -166,14 +166,14 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
 // The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
 // list the groups and their logits.
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 4;
-template <int TOK, bool TOP>
+template <int TOK, bool TOP, int PER>            // PER: groups of a tile
 __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tile, const float* __restrict__ Z,
                                                                   int64_t ldz, TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
     constexpr int GROUPS = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;      // lane groups of the tiles; wavefronts per token
     constexpr int ROW = TOK + 1;                                            // maxima in LDS: row pitch, tiles of a block
-    constexpr int BLOCK = JOIN_MAXIMA / TOK / STATS_GROUPS;
-    static_assert(STATS_GROUPS == 2, "maxima of a tile");
-    __shared__ float maxima[TOP ? STATS_GROUPS * BLOCK * ROW : 1];
+    constexpr int BLOCK = JOIN_MAXIMA / TOK / PER;
+    static_assert(PER == 1 || PER == 2, "maxima of a tile");
+    __shared__ float maxima[TOP ? PER * BLOCK * ROW : 1];
     __shared__ Stats red[JOIN_WAVES][TOK];
     __shared__ Stats fin[TOK];
     __shared__ uint64_t lists[TOP && WPT > 1 ? JOIN_WAVES : 1][TOP_MAX];
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
     const int tok = tid % TOK, group = tid / TOK, n = blockIdx.x * TOK + tok;
     const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
     const Stats none = no_stats();
-    const int tiles = (a.V + tile - 1) / tile, rows = tile / STATS_GROUPS, groups = (a.V + rows - 1) / rows;
+    const int tiles = (a.V + tile - 1) / tile, rows = tile / PER, groups = (a.V + rows - 1) / rows;
     Stats s = none;
     TopList top;
     for (int b0 = 0; b0 < tiles; b0 += BLOCK) {
@@ -195,8 +195,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
                     const int t = t0 + u * GROUPS;
                     if (t >= b1) break;
-                    m0[u] = part.mx[(size_t)(2 * t) * part.pitch + n];
-                    m1[u] = part.mx[(size_t)(2 * t + 1) * part.pitch + n];
+                    m0[u] = part.mx[(size_t)(PER * t) * part.pitch + n];
+                    m1[u] = PER == 2 ? part.mx[(size_t)(PER * t + 1) * part.pitch + n] : m0[u];
                     sd[u] = part.sd[(size_t)t * part.pitch + n];
                 }
 #pragma unroll
@@ -205,8 +205,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
                     if (t >= b1) break;
                     s = join(s, Stats{fmaxf(m0[u], m1[u]), sd[u].x, sd[u].y});
                     if (TOP) {
-                        maxima[(2 * (t - b0)) * ROW + tok] = m0[u];
-                        maxima[(2 * (t - b0) + 1) * ROW + tok] = m1[u];
+                        maxima[(PER * (t - b0)) * ROW + tok] = m0[u];
+                        if (PER == 2) maxima[(PER * (t - b0) + 1) * ROW + tok] = m1[u];
                     }
                 }
             }
@@ -214,16 +214,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
         if (!TOP) continue;
         __syncthreads();
         if (my_n < cv.n_c) {
-            const int g1 = 2 * b1 < groups ? 2 * b1 : groups;
+            const int g1 = PER * b1 < groups ? PER * b1 : groups;
             if (b0 == 0 && g1 > 128) {
                 // the lanes' own maxima bound what is listed: a quarter more than k instead of k (1 + log(groups / k))
                 float m = -__builtin_inff();
                 for (int g = sub * 64 + lane; g < g1; g += WPT * 64) m = fmaxf(m, maxima[g * ROW + my_tok]);
                 top.at_least(kth_of_lanes(m, o.top_k, lane));
             }
-            for (int g0 = 2 * b0 + sub * 64; g0 < g1; g0 += WPT * 64) {
+            for (int g0 = PER * b0 + sub * 64; g0 < g1; g0 += WPT * 64) {
                 const int g = g0 + lane;
-                top.offer(g < g1 ? top_key(maxima[(g - 2 * b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
+                top.offer(g < g1 ? top_key(maxima[(g - PER * b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
             }
         }
     }
@@ -411,9 +411,15 @@ void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int6
     auto go = [&](auto tok) {
         constexpr int TOK = decltype(tok)::value;
         const unsigned blocks = (unsigned)ceil_div(cv.n_c, TOK);
-        if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
-        else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        if (o.top_k > 0) stats_join_kernel<TOK, true, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<TOK, false, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
     };
+    if (logits_tile_groups(tile) == 1) {
+        const unsigned blocks = (unsigned)ceil_div(cv.n_c, 4);
+        if (o.top_k > 0) stats_join_kernel<4, true, 1><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<4, false, 1><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        return;
+    }
     // As many tokens a workgroup as leave every compute unit at most one, from 4 on. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens
     // 25.6 / 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83; one token 15.5 / 19.6 / 28.4 (1 token a workgroup 17.7).
     if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});

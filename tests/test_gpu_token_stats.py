@@ -108,6 +108,8 @@ def check_stats(out, z, y, k, z_err=0.0):
     ("bf16", 1, 64, 1, 1), ("bf16", 1, 128, 20011, 20), ("bf16", 2, 64, 257, 64), ("bf16", 95, 64, 700, 3), ("bf16", 97, 128, 256, 8),
     ("bf16", 128, 192, 1000, 0), ("bf16", 129, 64, 513, 20), ("bf16", 192, 256, 4099, 5), ("bf16", 193, 64, 300, 1),
     ("bf16", 256, 64, 64, 64), ("bf16", 257, 128, 20011, 20), ("bf16", 700, 512, 2049, 33), ("bf16", 520, 64, 33333, 64),
+    ("bf16", 5, 1088, 700, 4), ("bf16", 16, 2560, 1003, 20), ("bf16", 3, 4096, 515, 3), ("bf16", 3, 4160, 515, 3), ("bf16", 17, 2560, 300, 3),
+    ("i8", 7, 2176, 700, 4), ("i8", 16, 6144, 333, 20), ("i8", 4, 6272, 333, 5), ("i8", 2, 1024, 33000, 64),
     ("bf16", 300, 64, 70001, 20), ("bf16", 300, 128, 20011, 3), ("bf16", 1500, 64, 16700, 1), ("i8", 300, 128, 70001, 20),
     ("i8", 1, 128, 1, 1), ("i8", 1, 128, 20011, 20), ("i8", 50, 256, 1000, 7), ("i8", 100, 128, 300, 0), ("i8", 150, 384, 513, 64),
     ("i8", 192, 128, 4099, 2), ("i8", 193, 128, 255, 20), ("i8", 513, 256, 20011, 20), ("i8", 300, 1152, 257, 9)])
@@ -464,7 +466,7 @@ def test_quantize_rows_of_odd_values(P):
     assert P.dppo_quantize_rows(x[:0])[0].shape == (0, 128)
 
 
-@pytest.mark.parametrize("T,D,V", [(1, 128, 1), (1, 4096, 5000), (3, 256, 257), (96, 128, 255), (97, 384, 1000), (128, 128, 128),
+@pytest.mark.parametrize("T,D,V", [(1, 128, 1), (1, 4096, 5000), (16, 6144, 100), (3, 6272, 100), (9, 1152, 70001), (3, 256, 257), (96, 128, 255), (97, 384, 1000), (128, 128, 128),
                                    (129, 128, 513), (192, 640, 300), (193, 128, 1001), (256, 256, 512), (700, 1152, 2001)])
 @pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
 def test_matmul_i8(P, T, D, V, out):
