@@ -411,14 +411,16 @@ I8_ROW = 128       # rows of int8 operands are padded with zeros to a multiple o
 _STATS_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int8: 2}
 
 
+# The smallest calls are bound by what happens here before their launches: each check is a few attribute comparisons, and a tensor that
+# passed is handed on by its address alone.
 def _arg(t, name: str, dtype, shape: tuple, device):
-    """A checked tensor argument (None passes): the library reads and writes what these say and no more."""
+    """The address of a checked tensor argument (None: NULL): the library reads and writes what these say and no more."""
     if t is None:
         return None
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s on %s (got %s %s on %s)"
-                         % (name, dtype, shape, device, t.dtype, tuple(t.shape), t.device))
-    return t
+                         % (name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
 
 
 class _on_device:
@@ -438,23 +440,28 @@ class _on_device:
             self.guard.__exit__(*exc)
 
 
-def _stats_shape(H, W, ids, loss_pos, status) -> HeadShape:
-    if H.dtype not in _STATS_DTYPES or H.dim() != 2 or W.dim() != 2:
+def _stats_args(H, W, ids, loss_pos, status):
+    """The shape, and the addresses of the checked arguments."""
+    code = _STATS_DTYPES.get(H.dtype)
+    if code is None or H.dim() != 2 or W.dim() != 2:
         raise ValueError("H [T,D] and W [V,D] must be float32, bfloat16 or int8 matrices")
     T, D = H.shape
-    _arg(H, "H", H.dtype, (T, D), H.device)
-    _arg(W, "W", H.dtype, (W.shape[0], D), H.device)
-    _arg(ids, "ids", torch.int32, (T,), H.device)
+    V = W.shape[0]
+    device = H.device
+    N = T
     if loss_pos is not None:
-        _arg(loss_pos, "loss_pos", torch.int32, (loss_pos.numel(),), H.device)
-    _arg(status, "status", torch.int32, (1,), H.device)
-    return HeadShape(T, T if loss_pos is None else loss_pos.numel(), D, W.shape[0], _STATS_DTYPES[H.dtype])
+        N = loss_pos.numel()
+    ptrs = (_arg(H, "H", H.dtype, H.shape, device), _arg(W, "W", H.dtype, (V, D), device),
+            _arg(ids, "ids", torch.int32, (T,), device), _arg(loss_pos, "loss_pos", torch.int32, (N,), device),
+            _arg(status, "status", torch.int32, (1,), device))
+    return HeadShape(T, N, D, V, code), ptrs
 
 
 def _stats_workspace(ws, shape, top_k, what, device) -> torch.Tensor:
     if ws is None:
-        return alloc_workspace(load().dppo_token_stats_workspace_bytes(ctypes.byref(shape), top_k, what), device)
-    return _arg(ws, "ws", torch.uint8, (ws.numel(),), device)
+        return torch.empty(max(256, _lib.dppo_token_stats_workspace_bytes(shape, top_k, what)), dtype=torch.uint8, device=device)
+    _arg(ws, "ws", torch.uint8, (ws.numel(),), device)
+    return ws
 
 
 def dppo_token_stats_workspace_bytes(T: int, N: int, D: int, V: int, dtype_code: int, top_k: int = 0,
@@ -475,25 +482,32 @@ def dppo_token_stats(H, W, ids=None, loss_pos=None, top_k: int = 0, h_scale=None
     """H [T,D], W [V,D] float32, bfloat16, or int8 with h_scale [T] and w_scale [V] (dppo_quantize_rows); ids [T] int32
     or None (no logp). Returns dict(logp[N] or None, lse[N], entropy[N], top_ids[N,top_k] and top_logp[N,top_k], None for
     top_k = 0) of device tensors; status: see dppo_token_logprob."""
-    lib = load()
+    lib = _lib or load()
     device = H.device
-    shape = _stats_shape(H, W, ids, loss_pos, status)
+    shape, (H_, W_, ids_, loss_pos_, status_) = _stats_args(H, W, ids, loss_pos, status)
     N = shape.N
-    _arg(h_scale, "h_scale", torch.float32, (shape.T,), device)
-    _arg(w_scale, "w_scale", torch.float32, (shape.V,), device)
+    scales = (_arg(h_scale, "h_scale", torch.float32, (shape.T,), device), _arg(w_scale, "w_scale", torch.float32, (shape.V,), device))
     with _on_device(device):
         ws = _stats_workspace(ws, shape, top_k, 0, device)
-        rooms = [N + 3 & -4] * 3
-        lse, entropy, logp = _pieces(torch.empty(sum(rooms), dtype=torch.float32, device=device), [N] * 3, rooms)
+        # one allocation for the results, each of which begins at a multiple of 16 bytes (4-byte words all of them)
+        room, k = N + 3 & -4, top_k if 0 < top_k <= TOP_K_MAX else 0
+        room_k = N * k + 3 & -4
+        buf = torch.empty(3 * room + 2 * room_k, dtype=torch.float32, device=device)
+        at = buf.data_ptr() if N else None
+        logp = top_ids = top_logp = None
+        if k:
+            lse, entropy, logp, top_logp, top_ids = _pieces(buf, [N] * 3 + [N * k] * 2, [room] * 3 + [room_k] * 2)
+            top_logp = top_logp.view(N, k)
+            top_ids = top_ids.view(torch.int32).view(N, k)
+        else:
+            lse, entropy, logp = _pieces(buf, [N] * 3, [room] * 3)
         if ids is None:
             logp = None
-        top_ids = top_logp = None
-        if top_k > 0:
-            top_ids = torch.empty((N, top_k), dtype=torch.int32, device=device)
-            top_logp = torch.empty((N, top_k), dtype=torch.float32, device=device)
-        st = lib.dppo_token_stats(ctypes.byref(shape), top_k, _ptr(H), _ptr(W), _ptr(h_scale), _ptr(w_scale), _ptr(ids),
-                                  _ptr(loss_pos), _ptr(logp), _ptr(lse), _ptr(entropy), _ptr(top_ids), _ptr(top_logp),
-                                  _ptr(status), _ptr(ws), ws.numel(), _stream(device))
+        base = at or 0
+        st = lib.dppo_token_stats(shape, top_k, H_, W_, scales[0], scales[1], ids_, loss_pos_,
+                                  base + 8 * room if ids is not None else None, at, base + 4 * room,
+                                  base + 12 * room + 4 * room_k if k else None, base + 12 * room if k else None,
+                                  status_, ws.data_ptr(), ws.numel(), _stream(device))
         _check(st, "dppo_token_stats")
     return dict(logp=logp, lse=lse, entropy=entropy, top_ids=top_ids, top_logp=top_logp)
 
@@ -504,32 +518,31 @@ def dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy=None, g_logp=None, g_
                          status: Optional[torch.Tensor] = None) -> dict:
     """Gradients of a loss given its derivatives by logp, lse and entropy ([N] float32 each or None), with lse and entropy as
     dppo_token_stats returned them. Returns dict(dH[T,D], dW[V,D] of dW_dtype or of the buffer handed in)."""
-    lib = load()
+    lib = _lib or load()
     device = H.device
-    shape = _stats_shape(H, W, ids, loss_pos, status)
-    if H.dtype == torch.int8:
+    shape, (H_, W_, ids_, loss_pos_, status_) = _stats_args(H, W, ids, loss_pos, status)
+    if shape.dtype == 2:
         raise ValueError("H and W must be float32 or bfloat16")
-    for name, t in dict(lse=lse, entropy=entropy, g_logp=g_logp, g_lse=g_lse, g_entropy=g_entropy).items():
-        _arg(t, name, torch.float32, (shape.N,), device)
+    per_token = [_arg(t, name, torch.float32, (shape.N,), device) for name, t in
+                 (("lse", lse), ("entropy", entropy), ("g_logp", g_logp), ("g_lse", g_lse), ("g_entropy", g_entropy))]
     if dW is None:
         if accumulate_dW:
             raise ValueError("accumulate_dW needs the dW buffer to accumulate into")
     else:
         dW_dtype = dW.dtype
-        _arg(dW, "dW", dW_dtype, tuple(W.shape), device)
-    if dW_dtype not in (torch.float32, torch.bfloat16):
+        _arg(dW, "dW", dW_dtype, W.shape, device)
+    if dW_dtype is not torch.float32 and dW_dtype is not torch.bfloat16:
         raise ValueError("dW must be float32 or bfloat16")
-    _arg(dH, "dH", H.dtype, tuple(H.shape), device)
+    _arg(dH, "dH", H.dtype, H.shape, device)
     with _on_device(device):
-        ws = _stats_workspace(ws, shape, 0, 2 if dW_dtype == torch.bfloat16 else 1, device)
+        ws = _stats_workspace(ws, shape, 0, 2 if dW_dtype is torch.bfloat16 else 1, device)
         if dH is None:
             dH = torch.empty_like(H)
         if dW is None:
             dW = torch.empty(W.shape, dtype=dW_dtype, device=device)
         p = StatsGradParams(1 if accumulate_dW else 0, _STATS_DTYPES[dW_dtype])
-        st = lib.dppo_token_stats_bwd(ctypes.byref(shape), ctypes.byref(p), _ptr(H), _ptr(W), _ptr(ids), _ptr(loss_pos),
-                                      _ptr(lse), _ptr(entropy), _ptr(g_logp), _ptr(g_lse), _ptr(g_entropy), _ptr(dH), _ptr(dW),
-                                      _ptr(status), _ptr(ws), ws.numel(), _stream(device))
+        st = lib.dppo_token_stats_bwd(shape, p, H_, W_, ids_, loss_pos_, *per_token, dH.data_ptr(), dW.data_ptr(), status_,
+                                      ws.data_ptr(), ws.numel(), _stream(device))
         _check(st, "dppo_token_stats_bwd")
     return dict(dH=dH, dW=dW)
 
@@ -537,43 +550,41 @@ def dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy=None, g_logp=None, g_
 def dppo_quantize_rows(X: torch.Tensor):
     """X [rows, D] float32 or bfloat16 -> (q [rows, D rounded up to a multiple of 128] int8, padded with zeros,
     scale [rows] float32) with X ~ q[:, :D] * scale[:, None]."""
-    lib = load()
-    if X.dtype not in (torch.float32, torch.bfloat16) or X.dim() != 2:
+    lib = _lib or load()
+    code = _STATS_DTYPES.get(X.dtype, 2)
+    if code == 2 or X.dim() != 2:
         raise ValueError("X must be a float32 or bfloat16 matrix")
     rows, D = X.shape
     device = X.device
-    _arg(X, "X", X.dtype, (rows, D), device)
+    X_ = _arg(X, "X", X.dtype, X.shape, device)
     pitch = (D + I8_ROW - 1) // I8_ROW * I8_ROW
     with _on_device(device):
         q = torch.empty((rows, pitch), dtype=torch.int8, device=device)
         scale = torch.empty(rows, dtype=torch.float32, device=device)
-        _check(lib.dppo_quantize_rows(rows, D, _STATS_DTYPES[X.dtype], _ptr(X), _ptr(q), pitch, _ptr(scale), _stream(device)),
-               "dppo_quantize_rows")
+        _check(lib.dppo_quantize_rows(rows, D, code, X_, q.data_ptr(), pitch, scale.data_ptr(), _stream(device)), "dppo_quantize_rows")
     return q, scale
 
 
 def dppo_matmul_i8(X, x_scale, W, w_scale, out_dtype: torch.dtype = torch.float32,
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X [T,D] int8 with x_scale [T], W [V,D] int8 with w_scale [V] -> Y [T,V] = X W^T * w_scale * x_scale, float32 or bfloat16."""
-    lib = load()
+    lib = _lib or load()
     device = X.device
     if X.dim() != 2 or W.dim() != 2:
         raise ValueError("X [T,D] and W [V,D] must be int8 matrices")
     (T, D), V = X.shape, W.shape[0]
-    _arg(X, "X", torch.int8, (T, D), device)
-    _arg(W, "W", torch.int8, (V, D), device)
-    _arg(x_scale, "x_scale", torch.float32, (T,), device)
-    _arg(w_scale, "w_scale", torch.float32, (V,), device)
+    X_, W_ = _arg(X, "X", torch.int8, X.shape, device), _arg(W, "W", torch.int8, (V, D), device)
+    xs_, ws_ = _arg(x_scale, "x_scale", torch.float32, (T,), device), _arg(w_scale, "w_scale", torch.float32, (V,), device)
     if out is not None:
         out_dtype = out.dtype
         _arg(out, "out", out_dtype, (T, V), device)
-    if out_dtype not in (torch.float32, torch.bfloat16):
+    if out_dtype is not torch.float32 and out_dtype is not torch.bfloat16:
         raise ValueError("the result is float32 or bfloat16")
     with _on_device(device):
         if out is None:
             out = torch.empty((T, V), dtype=out_dtype, device=device)
-        _check(lib.dppo_matmul_i8(T, V, D, _ptr(X), _ptr(x_scale), _ptr(W), _ptr(w_scale), _ptr(out), _STATS_DTYPES[out_dtype],
-                                  _stream(device)), "dppo_matmul_i8")
+        _check(lib.dppo_matmul_i8(T, V, D, X_, xs_, W_, ws_, out.data_ptr(), _STATS_DTYPES[out_dtype], _stream(device)),
+               "dppo_matmul_i8")
     return out
 
 

@@ -151,11 +151,11 @@ struct FewScales : OperandTag<I8> {
 template <bool I8, class Out>
 struct FewOut : FewScales<I8> {
     struct State {};
-    Out* C; int64_t ldc; int vec;
+    Out* C; int64_t ldc;
     __device__ __forceinline__ FewToken token(int, int64_t row) const { return FewToken{I8 ? this->s.h[row] : 1.0f, -1}; }
     template <class Acc>
     __device__ __forceinline__ void block(State&, const Acc& acc, int v, int t, int V, int n, const FewToken* tok, const float* scales) const {
-        if (t < n) store_logits(C + (size_t)t * ldc + v, this->logits(acc, tok[t].h, scales), vec && v + 4 <= V, V - v);
+        if (t < n) store_logits(C + (size_t)t * ldc + v, this->logits(acc, tok[t].h, scales), V - v);
     }
     __device__ __forceinline__ void finish(const State&, int, int, int) const {}
 };
@@ -281,7 +281,6 @@ void launch_logits_out(const LogitsOut& g, const OperandScales& s, int cus, hipS
     auto fill = [&](auto& e) {
         e.C = reinterpret_cast<Out*>(g.C);
         e.ldc = g.ldc;
-        e.vec = g.ldc % 4 == 0 && reinterpret_cast<uintptr_t>(g.C) % (4 * sizeof(Out)) == 0;
     };
     if (few_tokens(g.n, g.k2, I8)) {
         FewOut<I8, Out> e;

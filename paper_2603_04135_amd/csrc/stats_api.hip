@@ -208,7 +208,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         if (!few && (map || logp)) {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
             float* scale = reinterpret_cast<float*>(w + r.o_scale);
-            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr};
+            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0};
             launch_stats_gather(gr, cv, st);
             if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
@@ -269,7 +269,8 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
     char* w = reinterpret_cast<char*>(ws);
     {
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        launch_fill_zero(dH, (size_t)s.T * r.row_bytes, status, st);
+        // dH is cleared beside the first chunk's gathering, in one launch; the status word before it
+        launch_fill_zero(dH, s.N == 0 ? (size_t)s.T * r.row_bytes : 0, status, st);
         if (s.N == 0 && !p->accumulate_dW) launch_fill_zero(dW, (size_t)s.V * s.D * (dw16 ? 2 : 4), nullptr, st);
         if (s.N > 0 && s.dtype == BF16 && !r.direct_w) launch_transpose_w(W, s.V, s.D, r.Vp, w + r.o_wt, st);
     }
@@ -285,7 +286,8 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
         const ChunkView cv = view(n0, s.N, r.n_cp);
         {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-            launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, Hc, y, rowc, nullptr}, cv, st);
+            launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
+                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0}, cv, st);
         }
         StoreSpec oh{loss_pos ? dH : reinterpret_cast<char*>(dH) + (size_t)n0 * r.row_bytes, s.D, 0, loss_pos ? rowc : nullptr};
         StoreSpec ow{dw_sum, s.D, n0 == 0 && !p->accumulate_dW ? 0 : 1, nullptr};

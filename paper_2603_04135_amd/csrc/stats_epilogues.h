@@ -40,55 +40,82 @@ __device__ __forceinline__ void to_logits(Acc (&acc)[Cfg::MI][Cfg::NI], f32x4 (&
     }
 }
 
-// Four neighbouring logits of a token: one aligned store, or the first `left` of them one by one.
-template <class Out>
-__device__ __forceinline__ void store_logits(Out* dst, const f32x4& v, bool whole, int left) {
-    if constexpr (sizeof(Out) == 4) {
-        if (whole) { *reinterpret_cast<f32x4*>(dst) = v; return; }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) dst[j] = v[j];
-    } else {
-        const __bf16 b0 = (__bf16)v[0], b1 = (__bf16)v[1], b2 = (__bf16)v[2], b3 = (__bf16)v[3];
-        const uint16_t h[4] = {__builtin_bit_cast(uint16_t, b0), __builtin_bit_cast(uint16_t, b1), __builtin_bit_cast(uint16_t, b2),
-                               __builtin_bit_cast(uint16_t, b3)};
-        if (whole) { *reinterpret_cast<uint2*>(dst) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16); return; }
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j < left) dst[j] = h[j];
-    }
+// 16 bytes of results at any element's address (rows of any length follow each other).
+template <class Out> struct __attribute__((packed, aligned(sizeof(Out)))) Packed16 { Out x[16 / sizeof(Out)]; };
+
+__device__ __forceinline__ float as_out(float v, float) { return v; }
+__device__ __forceinline__ uint16_t as_out(float v, uint16_t) {
+    const __bf16 b = (__bf16)v;
+    return __builtin_bit_cast(uint16_t, b);
 }
 
-// Stores the logits, row-major by token: C[n, v]. A lane's four accumulators are four neighbouring vocabulary entries of one token,
-// one store where the pitch allows it.
+// Four neighbouring logits of a token: one store, or the first `left` of them one by one.
+template <class Out>
+__device__ __forceinline__ void store_logits(Out* dst, const f32x4& v, int left) {
+    struct __attribute__((packed, aligned(sizeof(Out)))) Four { Out x[4]; };
+    if (left >= 4) {
+        *reinterpret_cast<Four*>(dst) = Four{{as_out(v[0], Out()), as_out(v[1], Out()), as_out(v[2], Out()), as_out(v[3], Out())}};
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < left) dst[j] = as_out(v[j], Out());
+}
+
+// Stores the logits, row-major by token: C[n, v]. The tile goes through LDS as [token][vocabulary row], in as many parts as fit, and leaves
+// it in runs of whole tile rows, 16 bytes a lane: straight from the accumulators (32 or 64 bytes a token and instruction) 2047
+// tokens of D = 4096, V = 32000 in bfloat16 took 284 us instead of 235 (536 G products: 2.28 P/s).
 template <bool I8, class Out>
 struct EpiOut : OperandTag<I8> {
-    Out* C; int64_t ldc; int vec;          // vec: whole groups of four are aligned
+    Out* C; int64_t ldc;
     OperandScales scales;
 
+    template <class Cfg> static constexpr int pitch() { return Cfg::BM * (int)sizeof(Out) + 16; }
+    template <class Cfg> static constexpr int parts() { return Cfg::BN * pitch<Cfg>() <= 160 * 1024 ? 1 : 2; }
     __device__ __forceinline__ void look_up(int, int) const {}
     template <class Cfg, class Acc>
     __device__ __forceinline__ void run(Acc (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        constexpr int PITCH = pitch<Cfg>(), PARTS = parts<Cfg>(), WPP = Cfg::WGN / PARTS, TOKS = Cfg::BN / PARTS;
+        constexpr int PER = 16 / (int)sizeof(Out), CH = Cfg::BM / PER, RPP = Cfg::NT / CH;      // elements of a chunk, chunks of a row, rows of a pass
+        static_assert(Cfg::WGN % PARTS == 0 && TOKS % RPP == 0, "whole wavefronts, whole passes");
         f32x4 z[Cfg::MI][Cfg::NI];
         to_logits<Cfg>(acc, z, c, scales);
-        auto store = [&](auto full_tag) __attribute__((always_inline)) {
-            constexpr bool FULL = decltype(full_tag)::value;
 #pragma unroll
-            for (int ni = 0; ni < Cfg::NI; ++ni) {
-                const int n = c.n0 + ni * MB + acc_col(c.lane);
-                if (!FULL && n >= c.N) continue;
-                Out* dst = C + (size_t)n * ldc + c.m0 + acc_row(c.lane, 0);
+        for (int part = 0; part < PARTS; ++part) {
+            if (part > 0) __syncthreads();
+            if (c.wave_n / WPP == part) {
 #pragma unroll
-                for (int mi = 0; mi < Cfg::MI; ++mi)
-                    store_logits(dst + mi * MB, z[mi][ni], FULL, c.M - (c.m0 + mi * MB + acc_row(c.lane, 0)));
+                for (int ni = 0; ni < Cfg::NI; ++ni) {
+                    char* row = c.smem + ((c.wave_n % WPP) * Cfg::WTN + ni * MB + acc_col(c.lane)) * PITCH;
+#pragma unroll
+                    for (int mi = 0; mi < Cfg::MI; ++mi) {
+                        const f32x4 v = z[mi][ni];
+                        Out* dst = reinterpret_cast<Out*>(row) + c.wave_m * Cfg::WTM + mi * MB + acc_row(c.lane, 0);
+                        if constexpr (sizeof(Out) == 4) *reinterpret_cast<f32x4*>(dst) = v;
+                        else *reinterpret_cast<uint2*>(dst) = make_uint2(as_out(v[0], Out()) | (uint32_t)as_out(v[1], Out()) << 16,
+                                                                        as_out(v[2], Out()) | (uint32_t)as_out(v[3], Out()) << 16);
+                    }
+                }
             }
-        };
-        if (vec && c.bm0 + Cfg::BM <= c.M && c.bn0 + Cfg::BN <= c.N) store(std::true_type{});
-        else store(std::false_type{});
+            __syncthreads();
+            const int ch = c.tid % CH, v0 = c.bm0 + ch * PER;
+#pragma unroll
+            for (int p = 0; p < TOKS / RPP; ++p) {
+                const int t = p * RPP + c.tid / CH, n = c.bn0 + part * TOKS + t;
+                if (n >= c.N || v0 >= c.M) continue;
+                const Out* src = reinterpret_cast<const Out*>(c.smem + t * PITCH) + ch * PER;
+                Out* dst = C + (size_t)n * ldc + v0;
+                if (v0 + PER <= c.M) {
+                    *reinterpret_cast<Packed16<Out>*>(dst) = *reinterpret_cast<const Packed16<Out>*>(src);
+                } else {
+                    for (int k = 0; v0 + k < c.M; ++k) dst[k] = src[k];
+                }
+            }
+        }
     }
 
     template <class Cfg>
-    static constexpr int lds_bytes() { return 0; }
+    static constexpr int lds_bytes() { return Cfg::BN / parts<Cfg>() * pitch<Cfg>(); }
     static constexpr bool SWAP = false;
 };
 

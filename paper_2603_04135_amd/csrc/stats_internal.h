@@ -48,6 +48,7 @@ void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, Ch
 struct GatherRows {
     TokenArgs tokens; size_t row_bytes; const float* scale;
     void* out; int32_t* y; int32_t* rowc; float* scale_out;
+    void* clear; size_t clear_bytes;        // cleared by further workgroups of the launch
 };
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st);
 

@@ -165,11 +165,12 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
 // ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
 // The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
 // list the groups and their logits.
-constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 4;
+constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240;
 template <int TOK, bool TOP, int PER>            // PER: groups of a tile
 __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tile, const float* __restrict__ Z,
                                                                   int64_t ldz, TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
     constexpr int GROUPS = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;      // lane groups of the tiles; wavefronts per token
+    constexpr int JOIN_UNROLL = PER == 1 ? 6 : 4;                           // loads under way
     constexpr int ROW = TOK + 1;                                            // maxima in LDS: row pitch, tiles of a block
     constexpr int BLOCK = JOIN_MAXIMA / TOK / PER;
     static_assert(PER == 1 || PER == 2, "maxima of a tile");
@@ -243,48 +244,46 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
     }
     if (!TOP) return;
     __syncthreads();
-    // every wavefront of a token ends with the token's list
-    auto share = [&](TopList& l) __attribute__((always_inline)) {
+    // the token's first wavefront ends with its list
+    if (WPT > 1) {
 #pragma unroll
         for (int d = 1; d < WPT; d *= 2) {
             if (d > 1) __syncthreads();
-            lists[wave][lane] = l.entry;
+            if (sub % (2 * d) == d) lists[wave][lane] = top.entry;
             __syncthreads();
-            l.merge(lists[wave ^ d][lane], lane);
+            if (sub % (2 * d) == 0) top.merge(lists[wave + d][lane], lane);
         }
-    };
-    if (WPT > 1) share(top);
+    }
+    if (sub != 0 || my_n >= cv.n_c) return;
+    // ... and reads the groups' logits: all loads of 8 rounds under way at once, one round a lane's float4
+    constexpr int ROUNDS = 8;
     TopList best;
-    if (my_n < cv.n_c) {
-        const int count = groups < o.top_k ? groups : o.top_k;
-        // the k-th largest maximum: k logits are no smaller
-        if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
-        const float* z = Z + (size_t)my_n * ldz;
-        // rows / 4 lanes read a group
-        const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
-        for (int i0 = sub * per; i0 < count; i0 += WPT * per * JOIN_UNROLL) {
-            float4 x[JOIN_UNROLL];
-            int v0[JOIN_UNROLL];
+    const int count = groups < o.top_k ? groups : o.top_k;
+    // the k-th largest maximum: k logits are no smaller
+    if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
+    const float* z = Z + (size_t)my_n * ldz;
+    // rows / 4 lanes read a group
+    const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
+    for (int i0 = 0; i0 < count; i0 += per * ROUNDS) {
+        float4 x[ROUNDS];
+        int v0[ROUNDS];
 #pragma unroll
-            for (int u = 0; u < JOIN_UNROLL; ++u) {
-                const int i = i0 + u * WPT * per + which;
-                const uint32_t g = ~(uint32_t)__shfl((int)(uint32_t)top.entry, i < count ? i : 0, 64);
-                v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
-                if (v0[u] < a.V) x[u] = *reinterpret_cast<const float4*>(z + v0[u]);
-            }
+        for (int u = 0; u < ROUNDS; ++u) {
+            const int i = i0 + u * per + which;
+            const uint32_t g = ~(uint32_t)__shfl((int)(uint32_t)top.entry, i < count ? i : 0, 64);
+            v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
+            if (v0[u] < a.V) x[u] = *reinterpret_cast<const float4*>(z + v0[u]);
+        }
 #pragma unroll
-            for (int u = 0; u < JOIN_UNROLL; ++u) {
-                const float xx[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+        for (int u = 0; u < ROUNDS; ++u) {
+            if (i0 + u * per >= count) break;
+            const float xx[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
 #pragma unroll
-                for (int q = 0; q < 4; ++q) best.offer(v0[u] + q < a.V ? top_key(xx[q], (uint32_t)(v0[u] + q)) : 0, o.top_k, lane);
-            }
+            for (int q = 0; q < 4; ++q)
+                best.offer(v0[u] + q < a.V ? top_key(xx[q], (uint32_t)(v0[u] + q)) : 0, o.top_k, lane);
         }
     }
-    if (WPT > 1) {
-        __syncthreads();
-        share(best);
-    }
-    if (my_n < cv.n_c && sub == 0) write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
+    write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
 }
 
 // tau[n]: one wavefront per token lists the maxima of the leading groups, read with neighbouring tokens side by side.
@@ -309,7 +308,18 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
 
 // A wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row (16-byte vectors, zero beyond
 // n_c) and its scale. Bound by HBM.
-__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv) {
+__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv, unsigned gather_blocks) {
+    if (blockIdx.x >= gather_blocks) {
+        // (clear is 4-byte aligned, the words in front of and behind the vectors one by one)
+        uint32_t* p = reinterpret_cast<uint32_t*>(g.clear);
+        const size_t words = g.clear_bytes / 4, head = (size_t)(-(reinterpret_cast<intptr_t>(p) / 4) & 3), lead = head < words ? head : words;
+        const size_t vectors = (words - lead) / 4, i0 = (size_t)(blockIdx.x - gather_blocks) * 256 + threadIdx.x;
+        uint4* v = reinterpret_cast<uint4*>(p + lead);
+        for (size_t i = i0; i < vectors; i += (size_t)(gridDim.x - gather_blocks) * 256) v[i] = make_uint4(0, 0, 0, 0);
+        if (i0 < lead) p[i0] = 0;
+        if (lead + vectors * 4 + i0 < words) p[lead + vectors * 4 + i0] = 0;
+        return;
+    }
     const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (n >= cv.n_cp) return;
     const bool valid = n < cv.n_c;
@@ -415,9 +425,9 @@ void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int6
         else stats_join_kernel<TOK, false, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
     };
     if (logits_tile_groups(tile) == 1) {
-        const unsigned blocks = (unsigned)ceil_div(cv.n_c, 4);
-        if (o.top_k > 0) stats_join_kernel<4, true, 1><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
-        else stats_join_kernel<4, false, 1><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        // few tokens with many groups: a workgroup each
+        if (o.top_k > 0) stats_join_kernel<1, true, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<1, false, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
         return;
     }
     // As many tokens a workgroup as leave every compute unit at most one, from 4 on. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens
@@ -432,7 +442,9 @@ void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, Ch
 }
 
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {
-    stats_gather_kernel<<<(unsigned)ceil_div(cv.n_cp, 4), 256, 0, st>>>(g, cv);
+    const unsigned blocks = (unsigned)ceil_div(cv.n_cp, 4);
+    const int64_t fill = ceil_div((int64_t)g.clear_bytes, 16 * 256 * 4);
+    stats_gather_kernel<<<blocks + (unsigned)(fill < 4096 ? fill : 4096), 256, 0, st>>>(g, cv, blocks);
 }
 
 void launch_stats_grad_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const StatsGrad& g, ChunkView cv, hipStream_t st) {
