@@ -261,7 +261,7 @@ hipError_t allow_few() {
 }
 template <bool I8>
 void launch_stats_tiles(const LogitsOut& g, const OperandScales& s, const StatsTiles& t, int cus, hipStream_t st) {
-    if (few_tokens(g.n, g.k2, I8)) {
+    if (g.tile == TILE_FEW) {
         FewStats<I8> e;
         e.s = s; e.part = t.part; e.tokens = t.tokens; e.n0 = t.cv.n0;
         e.Z = reinterpret_cast<float*>(g.C); e.ldz = g.ldc;
@@ -282,7 +282,7 @@ void launch_logits_out(const LogitsOut& g, const OperandScales& s, int cus, hipS
         e.C = reinterpret_cast<Out*>(g.C);
         e.ldc = g.ldc;
     };
-    if (few_tokens(g.n, g.k2, I8)) {
+    if (g.tile == TILE_FEW) {
         FewOut<I8, Out> e;
         fill(e);
         e.s = s;

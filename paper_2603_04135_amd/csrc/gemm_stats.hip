@@ -8,7 +8,7 @@ DeviceSetup g_setup;
 // Of the logits of a call with alternatives, an eighth of the vocabulary is stored whole, and of the rest what exceeds the bound found
 // there (some 15 % of the groups with 20 alternatives of 151936). 8191 tokens of D = 2560, GEMM and bound, lead of a quarter / an eighth /
 // a sixteenth / none 4545 / 4555 / 4618 / 4982 us (4435 without alternatives), 3000 tokens 1754 / 1731 / 1760 / -, 300 355 / 354 / 400 / 377.
-constexpr int LEAD_SHARE = 8;
+constexpr int LEAD_SHARE = 8, LEAD_ROUNDS = 10;
 typedef EpiStore<2> EpiStoreDW16;
 
 hipError_t allow_all() {
@@ -28,16 +28,19 @@ void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, int cus, hipStre
     launch_stats_tiles<false>(g, OperandScales{nullptr, nullptr, nullptr, 0}, t, cus, st);
 }
 
-int stats_lead_tiles(int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups) {
+int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups) {
     *groups = 0;
-    if (top_k == 0 || n <= STATS_MAP_TOKENS) return 0;
-    const int tiles_m = (int)ceil_div(V, CfgBig::BM), tiles_n = (int)ceil_div(n, CfgBig::BN);
+    if (top_k == 0 || tile != TILE_256x256) return 0;
+    const int tiles_m = (int)ceil_div(V, CfgBig::BM), tiles_n = (int)ceil_div(n, CfgBig::BN), tiles = tiles_m * tiles_n;
     const int bands = tiles_m / CfgBig::GROUP_M, band = CfgBig::GROUP_M * tiles_n;
     int lead = tiles_m / LEAD_SHARE / CfgBig::GROUP_M;
     // to the nearest whole rounds of the chip
     const int rounds = (lead * band + cus / 2) / cus;
     if (rounds > 0) lead = (rounds * cus + band / 2) / band;
     if (lead >= bands || lead * CfgBig::GROUP_M * STATS_GROUPS < 2 * top_k) return 0;
+    // a launch more may cost a round more: few rounds are only cut where it does not
+    auto in_rounds = [&](int t) { return (t + cus - 1) / cus; };
+    if (in_rounds(tiles) < LEAD_ROUNDS && in_rounds(lead * band) + in_rounds(tiles - lead * band) > in_rounds(tiles)) return 0;
     *groups = lead * CfgBig::GROUP_M * STATS_GROUPS;
     return lead * band;
 }

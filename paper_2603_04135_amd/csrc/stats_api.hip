@@ -39,8 +39,8 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
         r.o_hc = take(s.dtype == F32 ? 0 : n * r.row_bytes);
         r.o_scale = take(s.dtype == I8 ? n * 4 : 0);
         r.o_z = take(s.dtype == F32 || top_k > 0 ? n * r.Vp * 4 : 0);
-        // (at most 128 tokens in 128-row tiles, 16 in 32-row ones: no more pairs than 256 tokens in 256-row tiles)
-        const size_t pairs = s.dtype == F32 ? 0 : n * mfma_logits_row_tiles(s.V);
+        // (16 tokens in 32-row tiles and 128 in 128-row ones are no more pairs than 256 in 256-row ones)
+        const size_t large = n * mfma_logits_row_tiles(s.V), pairs = s.dtype == F32 ? 0 : large > SMALL_TILE_PAIRS ? large : SMALL_TILE_PAIRS;
         r.o_mx = take(pairs * STATS_GROUPS * 4);
         r.o_sd = take(pairs * sizeof(float2));
         r.o_tau = take(s.dtype == F32 ? 0 : n * 4);
@@ -199,13 +199,15 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
             launch_stats_rows(Z, r.Vp, tokens, out, cv, partial, st);
             continue;
         }
-        // Few tokens: the GEMM's columns read the rows through loss_pos, its epilogue looks the targets up. Many: both are gathered first.
-        const bool few = cv.n_c <= STATS_MAP_TOKENS;
+        // All tiles but the largest read the rows through loss_pos, and their epilogue looks the targets up. For the largest both are gathered first.
+        const int32_t k2 = (int32_t)(r.row_bytes / 2);
+        const int tile = logits_tile(cv.n_c, s.V, k2, s.dtype == I8);
+        const bool gather = tile == TILE_256x256;
         const char* rows = reinterpret_cast<const char*>(H) + (map ? 0 : (size_t)n0 * r.row_bytes);
-        LogitsOut g{W, s.V, (int32_t)(r.row_bytes / 2), rows, map ? s.T : (int64_t)cv.n_c, map, cv.n_c, top_k > 0 ? Z : nullptr, r.Vp};
+        LogitsOut g{tile, W, s.V, k2, rows, map ? s.T : (int64_t)cv.n_c, map, cv.n_c, top_k > 0 ? Z : nullptr, r.Vp};
         OperandScales sc{w_scale, h_scale ? h_scale + (map ? 0 : n0) : nullptr, map, (int32_t)g.h_rows};
         int32_t* y = reinterpret_cast<int32_t*>(w + r.o_y);
-        if (!few && (map || logp)) {
+        if (gather && (map || logp)) {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
             float* scale = reinterpret_cast<float*>(w + r.o_scale);
             GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0};
@@ -214,15 +216,15 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
         }
         StatsTiles t{{reinterpret_cast<float*>(w + r.o_mx), reinterpret_cast<float2*>(w + r.o_sd),
-                      logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, few ? cv.n_c : cv.n_cp},
-                     tokens, few ? nullptr : y, cv, nullptr, 0, -1};
+                      logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, gather ? cv.n_cp : cv.n_c},
+                     tokens, gather ? y : nullptr, cv, nullptr, 0, -1};
         auto gemm = [&]() {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
             if (s.dtype == BF16) launch_stats_bf16(g, t, cus, st);
             else launch_stats_i8(g, sc, t, cus, st);
         };
         int32_t groups = 0;
-        const int lead = stats_lead_tiles(s.V, cv.n_c, top_k, cus, &groups);
+        const int lead = stats_lead_tiles(tile, s.V, cv.n_c, top_k, cus, &groups);
         if (lead > 0) {
             float* tau = reinterpret_cast<float*>(w + r.o_tau);
             t.count = lead;
@@ -233,7 +235,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         }
         gemm();
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        launch_stats_join(t.part, logits_tile_rows(cv.n_c, g.k2, s.dtype == I8), Z, r.Vp, tokens, few, out, cv, st);
+        launch_stats_join(t.part, tile, Z, r.Vp, tokens, !gather, out, cv, st);
     }
     return check_launch("dppo_token_stats");
 }
@@ -367,7 +369,7 @@ int dppo_matmul_i8(int64_t T, int32_t V, int32_t D, const int8_t* X, const float
     constexpr int64_t CHUNK = 32768;
     for (int64_t n0 = 0; n0 < T; n0 += CHUNK) {
         const int32_t n = (int32_t)(T - n0 < CHUNK ? T - n0 : CHUNK);
-        LogitsOut g{W, V, D / 2, X + (size_t)n0 * D, n, nullptr, n,
+        LogitsOut g{logits_tile(n, V, D / 2, true), W, V, D / 2, X + (size_t)n0 * D, n, nullptr, n,
                     reinterpret_cast<char*>(Y) + (size_t)n0 * V * element_bytes(out_dtype), V};
         launch_logits_i8(g, OperandScales{w_scale, x_scale + n0, nullptr, n}, out_dtype == BF16, cus, st);
     }

@@ -294,16 +294,14 @@ struct EpiStatsGrad {
 }  // namespace mfma
 
 namespace {
-// The tile of the vocabulary GEMM by the number of tokens, as for the log-probabilities alone (see CfgFew): up to 192 tokens
-// columns that read the tokens' rows of H where they lie, through the map. Beyond, the rows are contiguous.
 template <class Epi>
 void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st, int first = 0, int count = -1) {
     auto mapped = [&](auto cfg) {
         launch<decltype(cfg), A_ROWS, WG_ROUNDS, B_MAP>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count, 1, -1, (int)g.h_rows, 0, g.map, 0);
     };
-    if (g.n <= 96) mapped(CfgFew<96>{});
-    else if (g.n <= 128) mapped(CfgFew<128>{});
-    else if (g.n <= STATS_MAP_TOKENS) mapped(CfgBig192{});
+    if (g.tile == TILE_128x96) mapped(CfgFew<96>{});
+    else if (g.tile == TILE_128x128) mapped(CfgFew<128>{});
+    else if (g.tile == TILE_256x192) mapped(CfgBig192{});
     else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count);
 }
 template <class Epi>

@@ -33,12 +33,12 @@ struct PartialStats {
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
 
-// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows (logits_tile_groups; a unit of the kernel for few tokens is one): mx[g * pitch + n] is group g's maximum for token n,
+// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows (a unit of the kernel for few tokens is one): mx[g * pitch + n] is group g's maximum for token n,
 // sd[t * pitch + n] = {sum, dev} of tile t against its own maximum; zy[n]: target logits (or NULL).
 constexpr int STATS_GROUPS = 2;
 struct StatsPart { float* mx; float2* sd; float* zy; int32_t pitch; };
-// Joins a token's tiles (tile: rows of one) and picks the top alternatives from the stored logits of the groups that can hold them.
-void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+// Joins a token's tiles (LogitsTile) and picks the top alternatives from the stored logits of the groups that can hold them.
+void launch_stats_join(const StatsPart& part, int tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st);
 // tau[n] = the top_k-th largest maximum of token n's first `groups` groups (at least top_k).
 void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, ChunkView cv, float* tau, hipStream_t st);
@@ -84,27 +84,44 @@ void launch_to_bf16(const float* src, void* dst, size_t n, hipStream_t st);
 struct OperandScales {
     const float* w; const float* h; const int32_t* map; int32_t rows;
 };
-// Logits of n tokens, C[n, V] = H W^T with pitch ldc. k2: bytes of an operand row / 2 (a multiple of 64). Row n of the tokens is row
-// map[n] (clamped to h_rows) of H, or n where map is NULL; a map needs n <= STATS_MAP_TOKENS.
+// Tile of the vocabulary GEMM, rows (vocabulary) x columns (tokens); FEW: the kernel for few tokens. All but the largest read the tokens' rows
+// of H through a map.
+enum LogitsTile { TILE_FEW = 0, TILE_128x96 = 1, TILE_128x128 = 2, TILE_256x192 = 3, TILE_256x256 = 4 };
+constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 = 8192, FEW_ROW_BYTES_I8 = 6144;
+inline int32_t tile_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile <= TILE_128x128 ? 128 : 256; }
+// Groups of rows of a tile that have a maximum of their own (see StatsPart).
+inline int32_t tile_groups(int tile) { return tile == TILE_FEW ? 1 : STATS_GROUPS; }
+// For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
+// kernel for few tokens hold. Up to 192 tokens as for the log-probabilities alone (see CfgFew). Beyond, tiles of 128 x 128, two per
+// compute unit, while large ones would fill no more than half the chip, or a second round of it less than a quarter.
+// Statistics of D = 512, 128 x 128 / 256 x 256: V = 4000, 500 tokens (32 large tiles) 9 / 17 us, 2000 (128) 13 / 18, 4000 (256) 24 / 21;
+// V = 40000, 500 tokens (314) 30 / 36; of D = 2560: 24 / 47, 42 / 53, 98 / 65; 98 / 112; 1000 tokens (628) 188 / 175.
+inline int logits_tile(int32_t n, int32_t V, int32_t k2, bool i8) {
+    if (n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16)) return TILE_FEW;
+    if (n <= 96) return TILE_128x96;
+    if (n <= 128) return TILE_128x128;
+    constexpr int64_t CHIP = 256;                 // compute units
+    const int64_t large = ceil_div(V, 256) * ceil_div(n, 256);
+    if (2 * large <= CHIP || (large > CHIP && 4 * large <= 5 * CHIP)) return TILE_128x128;
+    return n <= 192 ? TILE_256x192 : TILE_256x256;
+}
+// Most pairs of (tile, token) that 128 x 128 tiles beyond 128 tokens make: 5/4 of a chip of large tiles.
+constexpr size_t SMALL_TILE_PAIRS = 2 * 320 * 256;
+// Logits of n tokens, C[n, V] = H W^T with pitch ldc, by tiles of the given kind. k2: bytes of an operand row / 2 (a multiple of 64). Row n
+// of the tokens is row map[n] (clamped to h_rows) of H, or n where map is NULL, as it has to be for the largest tile.
 struct LogitsOut {
+    int tile;
     const void* W; int32_t V; int32_t k2;
     const void* H; int64_t h_rows; const int32_t* map; int32_t n;
     void* C; int64_t ldc;
 };
-constexpr int32_t STATS_MAP_TOKENS = 192;
-// Vocabulary rows of a tile for n tokens with operand rows of 2 k2 bytes, and the groups of rows that it is cut into: up to 16 tokens a
-// kernel of their own, with operand rows of up to 8 KB (8-bit operands 6 KB), which is what its registers hold.
-constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 = 8192, FEW_ROW_BYTES_I8 = 6144;
-inline bool few_tokens(int32_t n, int32_t k2, bool i8) { return n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16); }
-inline int32_t logits_tile_rows(int32_t n, int32_t k2, bool i8) { return few_tokens(n, k2, i8) ? FEW_TILE_ROWS : n <= 128 ? 128 : 256; }
-inline int32_t logits_tile_groups(int32_t tile) { return tile == FEW_TILE_ROWS ? 1 : STATS_GROUPS; }
 // The same GEMM with the statistics in its epilogue (C NULL: the logits are not stored; otherwise ldc holds whole tiles).
 // tau: of groups whose maximum does not exceed tau[n] the logits are not stored (NULL: all are). first, count: tiles of the launch in the
 // order of the walk (count < 0: to the last).
 struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkView cv; const float* tau; int first, count; };
 // Leading tiles of the walk, whole bands of rows from vocabulary entry 0 on, that a call with alternatives launches ahead of the rest
 // (0: none), and how many groups of rows they are.
-int stats_lead_tiles(int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups);
+int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups);
 int mfma_stats_setup(int* compute_units);
 int mfma_i8_setup(int* compute_units);
 void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, int cus, hipStream_t st);

@@ -416,15 +416,16 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
     else join_parts_kernel<false><<<(unsigned)cv.n_c, 64, 0, st>>>(Z, ldz, a, o, cv, partial);
 }
 
-void launch_stats_join(const StatsPart& part, int32_t tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+void launch_stats_join(const StatsPart& part, int tile_kind, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st) {
+    const int32_t tile = tile_rows(tile_kind);
     auto go = [&](auto tok) {
         constexpr int TOK = decltype(tok)::value;
         const unsigned blocks = (unsigned)ceil_div(cv.n_c, TOK);
         if (o.top_k > 0) stats_join_kernel<TOK, true, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
         else stats_join_kernel<TOK, false, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
     };
-    if (logits_tile_groups(tile) == 1) {
+    if (tile_groups(tile_kind) == 1) {
         // few tokens with many groups: a workgroup each
         if (o.top_k > 0) stats_join_kernel<1, true, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
         else stats_join_kernel<1, false, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
