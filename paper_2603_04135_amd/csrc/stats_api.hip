@@ -42,7 +42,7 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
         // (16 tokens in 32-row tiles and 128 in 128-row ones are no more pairs than 256 in 256-row ones)
         const size_t large = n * mfma_logits_row_tiles(s.V), pairs = s.dtype == F32 ? 0 : large > SMALL_TILE_PAIRS ? large : SMALL_TILE_PAIRS;
         r.o_mx = take(pairs * STATS_GROUPS * 4);
-        r.o_sd = take(pairs * sizeof(float2));
+        r.o_sd = take(pairs * STATS_GROUPS * sizeof(float2));
         r.o_tau = take(s.dtype == F32 ? 0 : n * 4);
         r.o_zy = take(s.dtype == F32 ? 0 : n * 4);
         r.o_y = take(s.dtype == F32 ? 0 : n * 4);
@@ -235,7 +235,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         }
         gemm();
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-        launch_stats_join(t.part, tile, Z, r.Vp, tokens, !gather, out, cv, st);
+        launch_stats_join(t.part, group_rows(tile), Z, r.Vp, tokens, !gather, out, cv, st);
     }
     return check_launch("dppo_token_stats");
 }

@@ -10,34 +10,48 @@ namespace mfma {
 template <bool I8> struct OperandTag {};
 template <> struct OperandTag<true> { typedef void Int8; };
 
-// The wavefront's accumulators as logits: as they are (bfloat16 operands), or sum * w[v] * h[row] with both scales applied in 32
-// bits, in this order (8-bit operands; the sum itself is exact and is rounded once, to 32 bits).
-template <class Cfg, class Acc>
-__device__ __forceinline__ void to_logits(Acc (&acc)[Cfg::MI][Cfg::NI], f32x4 (&z)[Cfg::MI][Cfg::NI], const TileCtx& c, const OperandScales& s) {
-    if constexpr (std::is_same<Acc, f32x4>::value) {
+// Scales of a wavefront's logits (8-bit operands): of its rows' blocks and of its columns.
+template <class Cfg> struct TileScales { f32x4 w[Cfg::MI]; float h[Cfg::NI]; };
+template <class Cfg>
+__device__ __forceinline__ TileScales<Cfg> load_scales(const TileCtx& c, const OperandScales& s) {
+    TileScales<Cfg> t;
+    struct __attribute__((packed, aligned(4))) Four { f32x4 x; };
 #pragma unroll
-        for (int mi = 0; mi < Cfg::MI; ++mi)
+    for (int ni = 0; ni < Cfg::NI; ++ni) {
+        const int n = c.n0 + ni * MB + acc_col(c.lane);
+        int row = n < c.N ? n : c.N - 1;
+        if (s.map) row = s.map[row];
+        t.h[ni] = s.h[row < 0 ? 0 : row < s.rows ? row : s.rows - 1];
+    }
+    if (c.bm0 + Cfg::BM <= c.M) {
 #pragma unroll
-            for (int ni = 0; ni < Cfg::NI; ++ni) z[mi][ni] = acc[mi][ni];
+        for (int mi = 0; mi < Cfg::MI; ++mi) t.w[mi] = reinterpret_cast<const Four*>(s.w + c.m0 + mi * MB + acc_row(c.lane, 0))->x;
     } else {
-        float h[Cfg::NI];
-#pragma unroll
-        for (int ni = 0; ni < Cfg::NI; ++ni) {
-            const int n = c.n0 + ni * MB + acc_col(c.lane);
-            int row = n < c.N ? n : c.N - 1;
-            if (s.map) row = s.map[row];
-            h[ni] = s.h[row < 0 ? 0 : row < s.rows ? row : s.rows - 1];
-        }
 #pragma unroll
         for (int mi = 0; mi < Cfg::MI; ++mi)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int v = c.m0 + mi * MB + acc_row(c.lane, j);
-                const float w = s.w[v < c.M ? v : c.M - 1];
-#pragma unroll
-                for (int ni = 0; ni < Cfg::NI; ++ni) z[mi][ni][j] = (float)acc[mi][ni][j] * w * h[ni];
+                t.w[mi][j] = s.w[v < c.M ? v : c.M - 1];
             }
     }
+    return t;
+}
+// The wavefront's accumulators as logits: as they are (bfloat16 operands), or sum * w[v] * h[row] with both scales applied in 32
+// bits, in this order (8-bit operands; the sum itself is exact and is rounded once, to 32 bits).
+template <class Cfg, class Acc>
+__device__ __forceinline__ void to_logits(Acc (&acc)[Cfg::MI][Cfg::NI], f32x4 (&z)[Cfg::MI][Cfg::NI], const TileScales<Cfg>& s) {
+#pragma unroll
+    for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            if constexpr (std::is_same<Acc, f32x4>::value) {
+                z[mi][ni] = acc[mi][ni];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) z[mi][ni][j] = (float)acc[mi][ni][j] * s.w[mi][j] * s.h[ni];
+            }
+        }
 }
 
 // 16 bytes of results at any element's address (rows of any length follow each other).
@@ -79,7 +93,9 @@ struct EpiOut : OperandTag<I8> {
         constexpr int PER = 16 / (int)sizeof(Out), CH = Cfg::BM / PER, RPP = Cfg::NT / CH;      // elements of a chunk, chunks of a row, rows of a pass
         static_assert(Cfg::WGN % PARTS == 0 && TOKS % RPP == 0, "whole wavefronts, whole passes");
         f32x4 z[Cfg::MI][Cfg::NI];
-        to_logits<Cfg>(acc, z, c, scales);
+        TileScales<Cfg> ts;
+        if constexpr (I8) ts = load_scales<Cfg>(c, scales);
+        to_logits<Cfg>(acc, z, ts);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
             if (part > 0) __syncthreads();
@@ -119,28 +135,57 @@ struct EpiOut : OperandTag<I8> {
     static constexpr bool SWAP = false;
 };
 
-// Softmax statistics of every token over the tile's vocabulary rows (see Stats and StatsPart), in registers and combined across the
-// wavefronts through LDS; the target's logit from the accumulator that holds it; with STORE the logits that may be among the top
-// alternatives, row-major by token. A group (the rows of one wavefront) is stored for the tokens whose bound tau its maximum exceeds:
-// top_k groups of lower vocabulary entries reach tau, so nothing else can be among the alternatives (an equal logit loses to theirs).
+// Softmax statistics of every token over a wavefront's vocabulary rows (a group, see Stats and StatsPart), in registers; the target's logit
+// from the accumulator that holds it; with STORE the logits that may be among the top alternatives, row-major by token. A group is
+// stored for the tokens whose bound tau its maximum exceeds: top_k groups of lower vocabulary entries reach tau, so nothing else can be
+// among the alternatives (an equal logit loses to theirs).
+// (Nothing goes through LDS, so a resident workgroup could load its next tile's first slices meanwhile; it was slower: 8191 tokens of
+// D = 2560, V = 151936 4.68 against 4.55 ms, as the 256 registers do not hold both and the tiles that share panels drift apart.)
 template <bool I8, bool STORE>
 struct EpiStats : OperandTag<I8> {
     StatsPart part;
     OperandScales scales;
-    // y[n]: targets looked up before, or NULL: from tokens.ids (NULL: no targets)
+    // y[n]: targets looked up before, or NULL: from tokens.ids
     TokenArgs tokens; const int32_t* y; int64_t n0; int n_c;
     float* Z; int64_t ldz; const float* tau;
 
+    template <class Cfg> struct Pre { int at[Cfg::NI]; float tau[Cfg::NI]; TileScales<Cfg> scales; };
+    // What the epilogue needs from memory, all loads at once: targets relative to the wavefront's rows, bounds, scales.
+    template <class Cfg>
+    __device__ __forceinline__ Pre<Cfg> preload(const TileCtx& c) const {
+        Pre<Cfg> p;
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            const int n = c.n0 + ni * MB + acc_col(c.lane);
+            p.at[ni] = -1;
+            p.tau[ni] = -__builtin_inff();
+            if (n < n_c) {
+                if (part.zy) {
+                    int32_t t;
+                    if (y) {
+                        t = y[n];
+                    } else {
+                        int64_t row;
+                        locate_token(tokens.ids, tokens.loss_pos, tokens.T, tokens.V, n0 + n, row, t);
+                    }
+                    p.at[ni] = t - c.m0;
+                }
+                if (STORE && tau) p.tau[ni] = tau[n];
+            }
+        }
+        if constexpr (I8) p.scales = load_scales<Cfg>(c, scales);
+        return p;
+    }
     __device__ __forceinline__ void look_up(int, int) const {}
     template <class Cfg, class Acc>
     __device__ __forceinline__ void run(Acc (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        const Pre<Cfg> pre = preload<Cfg>(c);
         constexpr int MI = Cfg::MI, NI = Cfg::NI;
         const float NEG_INF = -__builtin_inff();
         f32x4 z[MI][NI];
-        to_logits<Cfg>(acc, z, c, scales);
+        to_logits<Cfg>(acc, z, pre.scales);
         static_assert(Cfg::WGM == STATS_GROUPS, "a wavefront's rows = a group");
-        float* mx_out = part.mx + (size_t)(c.tm * STATS_GROUPS + c.wave_m) * part.pitch;
-        float3* red = reinterpret_cast<float3*>(c.smem);
+        const size_t g = (size_t)(c.tm * STATS_GROUPS + c.wave_m) * part.pitch;
         auto reduce = [&](auto full_tag) __attribute__((always_inline)) {
             constexpr bool FULL = decltype(full_tag)::value;
 #pragma unroll
@@ -156,10 +201,10 @@ struct EpiStats : OperandTag<I8> {
                 m = fmaxf(m, __shfl_xor(m, 16, 64));
                 m = fmaxf(m, __shfl_xor(m, 32, 64));
                 const int n = c.n0 + ni * MB + acc_col(c.lane);
-                if (n < n_c) {
-                    if (c.lane < MB) mx_out[n] = m;
+                if (STORE) {
                     // whole groups, the padding of the vocabulary too (the pitch holds it)
-                    if (STORE && (!tau || m > tau[n])) {
+                    const bool store = n < n_c && (!tau || m > pre.tau[ni]);
+                    if (store) {
                         float* dst = Z + (size_t)n * ldz + c.m0 + acc_row(c.lane, 0);
 #pragma unroll
                         for (int mi = 0; mi < MI; ++mi) *reinterpret_cast<f32x4*>(dst + mi * MB) = z[mi][ni];
@@ -179,7 +224,10 @@ struct EpiStats : OperandTag<I8> {
                 sum += __shfl_xor(sum, 32, 64);
                 dev += __shfl_xor(dev, 16, 64);
                 dev += __shfl_xor(dev, 32, 64);
-                if (c.lane < MB) red[c.wave_m * Cfg::BN + c.wave_n * Cfg::WTN + ni * MB + c.lane] = make_float3(m, sum, dev);
+                if (c.lane < MB && n < n_c) {
+                    part.mx[g + n] = m;
+                    part.sd[g + n] = make_float2(sum, dev);
+                }
             }
         };
         if (c.bm0 + Cfg::BM <= c.M) reduce(std::true_type{});
@@ -187,43 +235,18 @@ struct EpiStats : OperandTag<I8> {
         if (part.zy) {
 #pragma unroll
             for (int ni = 0; ni < NI; ++ni) {
-                const int n = c.n0 + ni * MB + acc_col(c.lane);
-                int at = -1;                                        // target among the wavefront's rows
-                if (n < n_c) {
-                    int32_t t;
-                    if (y) {
-                        t = y[n];
-                    } else {
-                        int64_t row;
-                        locate_token(tokens.ids, tokens.loss_pos, tokens.T, tokens.V, n0 + n, row, t);
-                    }
-                    at = t - c.m0;
-                }
-                if (!__any(at >= 0 && at < Cfg::WTM)) continue;
+                if (!__any(pre.at[ni] >= 0 && pre.at[ni] < Cfg::WTM)) continue;
 #pragma unroll
                 for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (at == mi * MB + acc_row(c.lane, j)) part.zy[n] = z[mi][ni][j];
+                        if (pre.at[ni] == mi * MB + acc_row(c.lane, j)) part.zy[c.n0 + ni * MB + acc_col(c.lane)] = z[mi][ni][j];
             }
-        }
-        __syncthreads();
-        for (int t = c.tid; t < Cfg::BN; t += Cfg::NT) {
-            const int n = c.bn0 + t;
-            if (n >= n_c) continue;
-            Stats s = no_stats();
-#pragma unroll
-            for (int w = 0; w < Cfg::WGM; ++w) {
-                const float3 r = red[w * Cfg::BN + t];
-                s = join(s, Stats{r.x, r.y, r.z});
-            }
-            const size_t at = (size_t)c.tm * part.pitch + n;
-            part.sd[at] = make_float2(s.sum, s.dev);
         }
     }
 
     template <class Cfg>
-    static constexpr int lds_bytes() { return Cfg::WGM * Cfg::BN * 12; }
+    static constexpr int lds_bytes() { return 0; }
     static constexpr bool SWAP = false;
 };
 
@@ -302,7 +325,7 @@ void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st, int first =
     if (g.tile == TILE_128x96) mapped(CfgFew<96>{});
     else if (g.tile == TILE_128x128) mapped(CfgFew<128>{});
     else if (g.tile == TILE_256x192) mapped(CfgBig192{});
-    else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count);
+    else launch<CfgBig>(g.W, g.k2, g.H, g.k2, g.V, g.n, g.k2, e, st, first, count, 1, PHASE_LOGITS);
 }
 template <class Epi>
 hipError_t allow_logits() {

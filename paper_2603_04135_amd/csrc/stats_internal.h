@@ -33,12 +33,12 @@ struct PartialStats {
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
 
-// Statistics of the vocabulary GEMM. A row tile is STATS_GROUPS groups of rows (a unit of the kernel for few tokens is one): mx[g * pitch + n] is group g's maximum for token n,
-// sd[t * pitch + n] = {sum, dev} of tile t against its own maximum; zy[n]: target logits (or NULL).
+// Statistics of the vocabulary GEMM by groups of rows, STATS_GROUPS of a tile (a unit of the kernel for few tokens is one): mx[g * pitch + n]
+// is group g's maximum for token n, sd[g * pitch + n] = {sum, dev} against it; zy[n]: target logits (or NULL).
 constexpr int STATS_GROUPS = 2;
 struct StatsPart { float* mx; float2* sd; float* zy; int32_t pitch; };
-// Joins a token's tiles (LogitsTile) and picks the top alternatives from the stored logits of the groups that can hold them.
-void launch_stats_join(const StatsPart& part, int tile, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+// Joins a token's groups (of `rows` rows) and picks the top alternatives from the stored logits of the groups that can hold them.
+void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st);
 // tau[n] = the top_k-th largest maximum of token n's first `groups` groups (at least top_k).
 void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, ChunkView cv, float* tau, hipStream_t st);
@@ -89,8 +89,8 @@ struct OperandScales {
 enum LogitsTile { TILE_FEW = 0, TILE_128x96 = 1, TILE_128x128 = 2, TILE_256x192 = 3, TILE_256x256 = 4 };
 constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 = 8192, FEW_ROW_BYTES_I8 = 6144;
 inline int32_t tile_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile <= TILE_128x128 ? 128 : 256; }
-// Groups of rows of a tile that have a maximum of their own (see StatsPart).
-inline int32_t tile_groups(int tile) { return tile == TILE_FEW ? 1 : STATS_GROUPS; }
+// Rows of a group of a tile (see StatsPart).
+inline int32_t group_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile_rows(tile) / STATS_GROUPS; }
 // For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
 // kernel for few tokens hold. Up to 192 tokens as for the log-probabilities alone (see CfgFew). Beyond, tiles of 128 x 128, two per
 // compute unit, while large ones would fill no more than half the chip, or a second round of it less than a quarter.

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
     const int vectors = (a.V + 3) / 4;
     const int lo = (int)((int64_t)vectors * part / partial.parts), hi = (int)((int64_t)vectors * (part + 1) / partial.parts);
     Stats s = no_stats();
-    TopList top;
+    TopList top(lists[wave]);
     // (whole wavefronts walk the loop: the list needs every lane)
     for (int i0 = lo + wave * 64; i0 < hi; i0 += ROWS_THREADS * ROWS_UNROLL) {
         float x[ROWS_UNROLL][4], m4[ROWS_UNROLL];
@@ -104,7 +104,10 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
     }
     s = join_lanes(s);
     if (lane == 0) red[wave] = s;
-    if (TOP) lists[wave][lane] = top.entry;
+    if (TOP) {
+        top.flush(o.top_k, lane);
+        lists[wave][lane] = top.entry;
+    }
     __syncthreads();
     if (wave != 0) return;
     for (int w = 1; w < ROWS_WAVES; ++w) s = join(s, red[w]);
@@ -142,10 +145,12 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
         s = join(s, Stats{v.x, v.y, v.z});
     }
     s = join_lanes(s);
-    TopList top;
+    __shared__ uint64_t pending[TOP_MAX];
+    TopList top(pending);
     if (TOP) {
         const int entries = partial.parts * o.top_k;
         for (int i = 0; i < entries; i += 64) top.offer(i + lane < entries ? partial.keys[at * o.top_k + i + lane] : 0, o.top_k, lane);
+        top.flush(o.top_k, lane);
     }
     const int64_t gi = cv.n0 + n;
     float zy = 0.0f;
@@ -160,72 +165,64 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
     if (TOP) write_top(o, gi, s, top, lane);
 }
 
-// Joins the per-tile statistics of TOK tokens per workgroup, and picks their top alternatives. The k largest logits of a token lie in
-// the k groups with the largest maxima (in the order of maximum, then group: every group ahead of another one holds a logit that is
-// ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
+// Joins the statistics of TOK tokens per workgroup over the groups of rows, and picks their top alternatives. The k largest logits of a
+// token lie in the k groups with the largest maxima (in the order of maximum, then group: every group ahead of another one holds a
+// logit that is ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
 // The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
-// list the groups and their logits.
-constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240;
-template <int TOK, bool TOP, int PER>            // PER: groups of a tile
-__global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t tile, const float* __restrict__ Z,
-                                                                  int64_t ldz, TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
-    constexpr int GROUPS = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;      // lane groups of the tiles; wavefronts per token
-    constexpr int JOIN_UNROLL = PER == 1 ? 6 : 4;                           // loads under way
-    constexpr int ROW = TOK + 1;                                            // maxima in LDS: row pitch, tiles of a block
-    constexpr int BLOCK = JOIN_MAXIMA / TOK / PER;
-    static_assert(PER == 1 || PER == 2, "maxima of a tile");
-    __shared__ float maxima[TOP ? PER * BLOCK * ROW : 1];
+// list the groups, and the first of them their logits.
+constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 6;
+template <int TOK, bool TOP>
+__global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t rows, const float* __restrict__ Z, int64_t ldz,
+                                                                  TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
+    constexpr int LANES = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;       // lanes and wavefronts per token
+    constexpr int ROW = TOK + 1, BLOCK = JOIN_MAXIMA / TOK;                 // maxima in LDS: row pitch, groups of a block
+    __shared__ float maxima[TOP ? BLOCK * ROW : 1];
     __shared__ Stats red[JOIN_WAVES][TOK];
     __shared__ Stats fin[TOK];
-    __shared__ uint64_t lists[TOP && WPT > 1 ? JOIN_WAVES : 1][TOP_MAX];
+    __shared__ uint64_t lists[TOP ? JOIN_WAVES : 1][TOP_MAX];               // of the wavefronts: newcomers, then lists that are shared
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int tok = tid % TOK, group = tid / TOK, n = blockIdx.x * TOK + tok;
+    const int tok = tid % TOK, n = blockIdx.x * TOK + tok;
     const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
-    const Stats none = no_stats();
-    const int tiles = (a.V + tile - 1) / tile, rows = tile / PER, groups = (a.V + rows - 1) / rows;
-    Stats s = none;
-    TopList top;
-    for (int b0 = 0; b0 < tiles; b0 += BLOCK) {
-        const int b1 = tiles - b0 < BLOCK ? tiles : b0 + BLOCK;
+    const int groups = (a.V + rows - 1) / rows;
+    Stats s = no_stats();
+    TopList top(lists[TOP ? wave : 0]);
+    for (int b0 = 0; b0 < groups; b0 += BLOCK) {
+        const int b1 = groups - b0 < BLOCK ? groups : b0 + BLOCK;
         if (TOP && b0 > 0) __syncthreads();
         if (n < cv.n_c) {
-            for (int t0 = b0 + group; t0 < b1; t0 += GROUPS * JOIN_UNROLL) {
+            for (int g0 = b0 + tid / TOK; g0 < b1; g0 += LANES * JOIN_UNROLL) {
                 float2 sd[JOIN_UNROLL];
-                float m0[JOIN_UNROLL], m1[JOIN_UNROLL];
+                float m[JOIN_UNROLL];
 #pragma unroll
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
-                    const int t = t0 + u * GROUPS;
-                    if (t >= b1) break;
-                    m0[u] = part.mx[(size_t)(PER * t) * part.pitch + n];
-                    m1[u] = PER == 2 ? part.mx[(size_t)(PER * t + 1) * part.pitch + n] : m0[u];
-                    sd[u] = part.sd[(size_t)t * part.pitch + n];
+                    const int g = g0 + u * LANES;
+                    if (g >= b1) break;
+                    m[u] = part.mx[(size_t)g * part.pitch + n];
+                    sd[u] = part.sd[(size_t)g * part.pitch + n];
                 }
 #pragma unroll
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
-                    const int t = t0 + u * GROUPS;
-                    if (t >= b1) break;
-                    s = join(s, Stats{fmaxf(m0[u], m1[u]), sd[u].x, sd[u].y});
-                    if (TOP) {
-                        maxima[(PER * (t - b0)) * ROW + tok] = m0[u];
-                        if (PER == 2) maxima[(PER * (t - b0) + 1) * ROW + tok] = m1[u];
-                    }
+                    const int g = g0 + u * LANES;
+                    if (g >= b1) break;
+                    s = join(s, Stats{m[u], sd[u].x, sd[u].y});
+                    if (TOP) maxima[(g - b0) * ROW + tok] = m[u];
                 }
             }
         }
         if (!TOP) continue;
         __syncthreads();
         if (my_n < cv.n_c) {
-            const int g1 = PER * b1 < groups ? PER * b1 : groups;
-            if (b0 == 0 && g1 > 128) {
+            if (b0 == 0 && b1 > 128) {
                 // the lanes' own maxima bound what is listed: a quarter more than k instead of k (1 + log(groups / k))
                 float m = -__builtin_inff();
-                for (int g = sub * 64 + lane; g < g1; g += WPT * 64) m = fmaxf(m, maxima[g * ROW + my_tok]);
+                for (int g = sub * 64 + lane; g < b1; g += WPT * 64) m = fmaxf(m, maxima[g * ROW + my_tok]);
                 top.at_least(kth_of_lanes(m, o.top_k, lane));
             }
-            for (int g0 = PER * b0 + sub * 64; g0 < g1; g0 += WPT * 64) {
+            for (int g0 = b0 + sub * 64; g0 < b1; g0 += WPT * 64) {
                 const int g = g0 + lane;
-                top.offer(g < g1 ? top_key(maxima[(g - PER * b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
+                top.offer(g < b1 ? top_key(maxima[(g - b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
             }
+            if (b1 == groups) top.flush(o.top_k, lane);
         }
     }
 #pragma unroll
@@ -257,7 +254,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
     if (sub != 0 || my_n >= cv.n_c) return;
     // ... and reads the groups' logits: all loads of 8 rounds under way at once, one round a lane's float4
     constexpr int ROUNDS = 8;
-    TopList best;
+    TopList best(lists[wave]);
     const int count = groups < o.top_k ? groups : o.top_k;
     // the k-th largest maximum: k logits are no smaller
     if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
@@ -283,6 +280,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
                 best.offer(v0[u] + q < a.V ? top_key(xx[q], (uint32_t)(v0[u] + q)) : 0, o.top_k, lane);
         }
     }
+    best.flush(o.top_k, lane);
     write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
 }
 
@@ -290,9 +288,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
 constexpr int BOUND_TOK = 16, BOUND_BLOCK = 640;
 __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32_t groups, int32_t top_k, int32_t n_c, float* __restrict__ tau) {
     __shared__ float maxima[BOUND_BLOCK * (BOUND_TOK + 1)];
+    __shared__ uint64_t pending[16][TOP_MAX];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int tok = tid % BOUND_TOK, n = blockIdx.x * BOUND_TOK + tok, my_n = blockIdx.x * BOUND_TOK + wave;
-    TopList top;
+    TopList top(pending[wave]);
     for (int g0 = 0; g0 < groups; g0 += BOUND_BLOCK) {
         const int g1 = groups - g0 < BOUND_BLOCK ? groups : g0 + BOUND_BLOCK;
         if (g0 > 0) __syncthreads();
@@ -303,6 +302,7 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
         for (int i = g0; i < g1; i += 64)
             top.offer(i + lane < g1 && my_n < n_c ? top_key(maxima[(i + lane - g0) * (BOUND_TOK + 1) + wave], (uint32_t)(i + lane)) : 0, top_k, lane);
     }
+    top.flush(top_k, lane);
     if (lane == 0 && my_n < n_c) tau[my_n] = top_value(lane_value(top.entry, top_k - 1));
 }
 
@@ -416,24 +416,18 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
     else join_parts_kernel<false><<<(unsigned)cv.n_c, 64, 0, st>>>(Z, ldz, a, o, cv, partial);
 }
 
-void launch_stats_join(const StatsPart& part, int tile_kind, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
+void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st) {
-    const int32_t tile = tile_rows(tile_kind);
     auto go = [&](auto tok) {
         constexpr int TOK = decltype(tok)::value;
         const unsigned blocks = (unsigned)ceil_div(cv.n_c, TOK);
-        if (o.top_k > 0) stats_join_kernel<TOK, true, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
-        else stats_join_kernel<TOK, false, 2><<<blocks, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
+        if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
+        else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
     };
-    if (tile_groups(tile_kind) == 1) {
-        // few tokens with many groups: a workgroup each
-        if (o.top_k > 0) stats_join_kernel<1, true, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
-        else stats_join_kernel<1, false, 1><<<cv.n_c, JOIN_THREADS, 0, st>>>(part, tile, Z, ldz, a, look_up, o, cv);
-        return;
-    }
-    // As many tokens a workgroup as leave every compute unit at most one, from 4 on. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens
-    // 25.6 / 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83; one token 15.5 / 19.6 / 28.4 (1 token a workgroup 17.7).
-    if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
+    // As many tokens a workgroup as leave every compute unit at most one, from 4 on; one where there are few tokens with many groups. V = 151936,
+    // 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 25.6 / 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83.
+    if (cv.n_c <= FEW_TILE_TOKENS) go(std::integral_constant<int, 1>{});
+    else if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
     else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 16>{});
 }
