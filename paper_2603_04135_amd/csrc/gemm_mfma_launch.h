@@ -110,13 +110,14 @@ hipError_t allow_lds() {
 
 // dW[V, D] of a chunk by epilogue Epi (EpiStore<0>: float32, EpiStore<2>: bfloat16, overwritten): G is read k-major from its blocks.
 // The tiles of a sparsely filled last round are cut along K where `partial` is scratch for the partial tiles
-// (mfma_dw_partial_bytes), which a second kernel adds up. resident: at most one workgroup per compute unit, which walks the tiles.
+// (mfma_dw_partial_bytes), which a second kernel adds up; k_parts > 0: all tiles, fewer than compute units, into that many. resident: at
+// most one workgroup per compute unit, which walks the tiles.
 template <class Epi>
 void launch_dw_tiles(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, const Epi& e, float* partial,
-                     bool resident, hipStream_t st) {
+                     bool resident, hipStream_t st, int k_parts = 0) {
     const int tiles_m = (int)ceil_div(V, CfgGrad::BM), tiles_n = (int)ceil_div(D, CfgGrad::BN);
     const int tiles = tiles_m * tiles_n, tail = cus > 0 ? tiles % cus : 0;
-    const int parts = partial ? mfma_tail_parts(cus, tail, n_cp / CfgGrad::BK) : 1;
+    const int parts = k_parts > 0 ? k_parts : partial ? mfma_tail_parts(cus, tail, n_cp / CfgGrad::BK) : 1;
     const int workgroups = resident ? cus : 0;
     const int whole = parts == 1 ? tiles : tiles - tail;
     launch<CfgGrad, A_BLK_KM, WG_RANGES, B_BLK>(G, Vp, HcT, 0, V, D, n_cp, e, st, 0, whole, 1, PHASE_DW, 0, workgroups);

@@ -1,4 +1,5 @@
 // bfloat16 GEMMs of the token statistics and their gradient.
+#include "api_internal.h"
 #include "few_tokens.h"
 
 namespace dppo {
@@ -10,12 +11,18 @@ DeviceSetup g_setup;
 // a sixteenth / none 4545 / 4555 / 4618 / 4982 us (4435 without alternatives), 3000 tokens 1754 / 1731 / 1760 / -, 300 355 / 354 / 400 / 377.
 constexpr int LEAD_SHARE = 8, LEAD_ROUNDS = 10;
 typedef EpiStore<2> EpiStoreDW16;
+// Gradient entries of up to 64 tokens, or where large tiles fill at most half the chip, by tiles of 64 tokens. D = 1152, 64 / 256 tokens a
+// tile: 2 tokens, V = 20000 13 / 28 us; 1016, V = 1516 (24 large tiles) 14 / 32, V = 6000 (96) 27 / 32; 300, V = 15160 (120) 26 / 31;
+// 250, V = 40000 (157) 40 / 33.
+typedef PipeCfg<256, 64, 4, 2, 2, 4, 1> CfgGradFew;
+constexpr int GRAD_FEW_TILES = 128;
 
 hipError_t allow_all() {
     hipError_t e = allow_logits<EpiStats<false, false>>();
     if (e == hipSuccess) e = allow_logits<EpiStats<false, true>>();
     if (e == hipSuccess) e = allow_few<false, FewStats<false>>();
     if (e == hipSuccess) e = allow_lds<CfgBig, EpiStatsGrad>();
+    if (e == hipSuccess) e = allow_lds<CfgGradFew, EpiStatsGrad>();
     if (e == hipSuccess) e = allow_lds<CfgGrad, EpiStoreDW16, A_BLK_KM, WG_RANGES, B_BLK>();
     return e;
 }
@@ -48,13 +55,16 @@ int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int
 void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc, ChunkView cv, const int32_t* y, const StatsGrad& g, void* G,
                             int32_t Vp, hipStream_t st) {
     EpiStatsGrad e{y, g, cv.n0, cv.n_c, reinterpret_cast<uint16_t*>(G), Vp, V};
-    launch<CfgBig>(W, D, Hc, D, V, cv.n_cp, D, e, st);
+    if (cv.n_c <= CfgGradFew::BN || ceil_div(V, CfgBig::BM) * ceil_div(cv.n_c, CfgBig::BN) <= GRAD_FEW_TILES)
+        launch<CfgGradFew>(W, D, Hc, D, V, round_up32(cv.n_c, CfgGradFew::BN), D, e, st);
+    else
+        launch<CfgBig>(W, D, Hc, D, V, cv.n_cp, D, e, st);
 }
 
 void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
-                         hipStream_t st) {
+                         hipStream_t st, int k_parts) {
     EpiStoreDW16 e{nullptr, reinterpret_cast<uint16_t*>(dW), D, 0, nullptr, nullptr, nullptr};
-    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, n_cp <= 2 * CfgGrad::BK, st);
+    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, n_cp <= 2 * CfgGrad::BK, st, k_parts);
 }
 
 }  // namespace dppo

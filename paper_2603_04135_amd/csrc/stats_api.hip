@@ -210,7 +210,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         if (gather && (map || logp)) {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
             float* scale = reinterpret_cast<float*>(w + r.o_scale);
-            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0};
+            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0, nullptr, 0};
             launch_stats_gather(gr, cv, st);
             if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
@@ -286,10 +286,12 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
     float* dw_sum = dw16 && !one_chunk ? reinterpret_cast<float*>(w + r.o_dwacc) : reinterpret_cast<float*>(dW);
     for (int64_t n0 = 0; n0 < s.N; n0 += r.n_cp) {
         const ChunkView cv = view(n0, s.N, r.n_cp);
+        // dW sums over the chunk's tokens up to whole slices of its GEMM
+        const int32_t n_sum = round_up32(cv.n_c, GEMM_B_BLOCK_K);
         {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
             launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
-                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0}, cv, st);
+                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0, s.dtype == BF16 ? w + r.o_hct : nullptr, n_sum}, cv, st);
         }
         StoreSpec oh{loss_pos ? dH : reinterpret_cast<char*>(dH) + (size_t)n0 * r.row_bytes, s.D, 0, loss_pos ? rowc : nullptr};
         StoreSpec ow{dw_sum, s.D, n0 == 0 && !p->accumulate_dW ? 0 : 1, nullptr};
@@ -313,13 +315,7 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
             launch_mfma_stats_grad(W, s.V, s.D, Hc, cv, y, grad, G, r.Vp, st);
         }
-        // dW sums over the chunk's tokens up to whole slices of its GEMM
-        const int32_t n_sum = round_up32(cv.n_c, GEMM_B_BLOCK_K);
         float* partial = reinterpret_cast<float*>(w + r.o_dwpart);
-        {
-            StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-            launch_scale_transpose_bf16(Hc, nullptr, n_sum, s.D, w + r.o_hct, st);
-        }
         {
             StageTimer tm(DPPO_STAGE_DH_GEMM, st);
             // partial tiles of dH: where dW is overwritten just behind, its memory holds more of them than the workspace
@@ -327,11 +323,15 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
             int64_t floats = (int64_t)(mfma_dw_partial_bytes() / 4);
             const int64_t dw_floats = (int64_t)s.V * s.D / (dw16 && one_chunk ? 2 : 1);
             if (!ow.accumulate && dw_floats > floats) { dh_partial = dw_sum; floats = dw_floats; }
-            launch_mfma_dh(cus, G, r.Vp, r.direct_w ? nullptr : w + r.o_wt, W, s.V, cv.n_c, s.D, nullptr, oh, dh_partial, floats, st);
+            const int tiles = mfma_dh_tiles(cv.n_c, s.D);
+            launch_mfma_dh(cus, G, r.Vp, r.direct_w ? nullptr : w + r.o_wt, W, s.V, cv.n_c, s.D, nullptr, oh, dh_partial, floats, st,
+                           2 * tiles <= cus ? few_tiles_parts(cus, tiles, r.Vp / GEMM_B_BLOCK_K) : 0);
         }
         StageTimer tm(DPPO_STAGE_DW_GEMM, st);
-        if (dw16 && one_chunk) launch_mfma_dw_bf16(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, dW, partial, st);
-        else launch_mfma_dw(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, ow, partial, st);
+        const int dw_tiles = mfma_dh_tiles(s.V, s.D);
+        const int dw_parts = 2 * dw_tiles <= cus ? few_tiles_parts(cus, dw_tiles, n_sum / GEMM_B_BLOCK_K) : 0;
+        if (dw16 && one_chunk) launch_mfma_dw_bf16(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, dW, partial, st, dw_parts);
+        else launch_mfma_dw(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, ow, partial, st, dw_parts);
     }
     if (dw16 && !one_chunk && s.N > 0) {
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);

@@ -49,6 +49,8 @@ struct GatherRows {
     TokenArgs tokens; size_t row_bytes; const float* scale;
     void* out; int32_t* y; int32_t* rowc; float* scale_out;
     void* clear; size_t clear_bytes;        // cleared by further workgroups of the launch
+    // bfloat16: the rows' transpose [D, transpose_cols] in the blocked B-operand layout, zero from n_c on, by further workgroups too (NULL: none)
+    void* transpose; int32_t transpose_cols;
 };
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st);
 
@@ -132,7 +134,19 @@ void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc,
                             int32_t Vp, hipStream_t st);
 // launch_mfma_dw with a bfloat16 result, overwritten.
 void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
-                         hipStream_t st);
+                         hipStream_t st, int k_parts = 0);
+// Parts along K of a GEMM whose few tiles fill at most half the chip: least estimated time. A slice takes 1.1 us, a partial tile (512 KB
+// written and read) 0.13, the launch that sums them 4. Up to 256 partial tiles, as many as mfma_dw_partial_bytes() holds, each of 4 slices
+// or more. dH of 6 tokens, D = 576, V = 1496 (3 tiles of 24 slices) whole 30 us, in 6 parts 13 and 4 for the sum.
+inline int few_tiles_parts(int cus, int tiles, int slices) {
+    int best = 1;
+    double best_t = 1.1 * slices;
+    for (int p = 2; p <= slices / 4 && tiles * p <= (cus < 256 ? cus : 256); ++p) {
+        const double t = 1.1 * ((slices + p - 1) / p) + 4.0 + 0.13 * tiles * p;
+        if (t < best_t) { best_t = t; best = p; }
+    }
+    return best;
+}
 
 // ---- 8-bit rows (quantize.hip) -------------------------------------------------
 void launch_quantize_rows(int dtype, const void* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float* scale, hipStream_t st);

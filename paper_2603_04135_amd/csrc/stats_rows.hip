@@ -308,16 +308,56 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
 
 // A wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row (16-byte vectors, zero beyond
 // n_c) and its scale. Bound by HBM.
-__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv, unsigned gather_blocks) {
-    if (blockIdx.x >= gather_blocks) {
+// Row of H of chunk token n, clamped (what is wrong with it is reported elsewhere).
+__device__ __forceinline__ int64_t token_row(const TokenArgs& a, ChunkView cv, int n) {
+    const int64_t row = a.loss_pos ? (int64_t)a.loss_pos[cv.n0 + n] : cv.n0 + n;
+    return row < 0 ? 0 : row >= a.T ? a.T - 1 : row;
+}
+// 64 tokens x 64 columns of the transpose through LDS, 16-byte accesses on both sides.
+__device__ void transpose_tokens(const GatherRows& g, ChunkView cv, int block, uint16_t (*tile)[64 + 2]) {
+    const int D = g.tokens.D, r0 = block / (D / 64) * 64, c0 = block % (D / 64) * 64;
+    const int vec = threadIdx.x & 7, line = threadIdx.x >> 3;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        const int rr = line + pass * 32, r = r0 + rr;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (r < cv.n_c) v = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(g.tokens.H) + (size_t)token_row(g.tokens, cv, r) * D + c0 + vec * 8);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            tile[rr][vec * 8 + 2 * k] = (uint16_t)(w[k] & 0xffffu);
+            tile[rr][vec * 8 + 2 * k + 1] = (uint16_t)(w[k] >> 16);
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        const int cc = line + pass * 32, drow = c0 + cc;
+        uint32_t w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[vec * 8 + 2 * k][cc] | ((uint32_t)tile[vec * 8 + 2 * k + 1][cc] << 16);
+        static_assert(GEMM_B_BLOCK_K == 64, "a 64-column tile = one block column");
+        const size_t off = ((size_t)(drow / GEMM_B_BLOCK_ROWS) * (g.transpose_cols / GEMM_B_BLOCK_K) + r0 / GEMM_B_BLOCK_K) *
+                               (GEMM_B_BLOCK_ROWS * GEMM_B_BLOCK_K) + (size_t)(drow % GEMM_B_BLOCK_ROWS) * GEMM_B_BLOCK_K + vec * 8;
+        *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.transpose) + off) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv, unsigned gather_blocks, unsigned transpose_blocks) {
+    __shared__ uint16_t tile[64][64 + 2];
+    if (blockIdx.x >= gather_blocks + transpose_blocks) {
         // (clear is 4-byte aligned, the words in front of and behind the vectors one by one)
         uint32_t* p = reinterpret_cast<uint32_t*>(g.clear);
+        const unsigned first = gather_blocks + transpose_blocks;
         const size_t words = g.clear_bytes / 4, head = (size_t)(-(reinterpret_cast<intptr_t>(p) / 4) & 3), lead = head < words ? head : words;
-        const size_t vectors = (words - lead) / 4, i0 = (size_t)(blockIdx.x - gather_blocks) * 256 + threadIdx.x;
+        const size_t vectors = (words - lead) / 4, i0 = (size_t)(blockIdx.x - first) * 256 + threadIdx.x;
         uint4* v = reinterpret_cast<uint4*>(p + lead);
-        for (size_t i = i0; i < vectors; i += (size_t)(gridDim.x - gather_blocks) * 256) v[i] = make_uint4(0, 0, 0, 0);
+        for (size_t i = i0; i < vectors; i += (size_t)(gridDim.x - first) * 256) v[i] = make_uint4(0, 0, 0, 0);
         if (i0 < lead) p[i0] = 0;
         if (lead + vectors * 4 + i0 < words) p[lead + vectors * 4 + i0] = 0;
+        return;
+    }
+    if (blockIdx.x >= gather_blocks) {
+        transpose_tokens(g, cv, (int)(blockIdx.x - gather_blocks), tile);
         return;
     }
     const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -438,8 +478,9 @@ void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, Ch
 
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {
     const unsigned blocks = (unsigned)ceil_div(cv.n_cp, 4);
+    const unsigned transposes = g.transpose ? (unsigned)(g.tokens.D / 64 * (g.transpose_cols / 64)) : 0;
     const int64_t fill = ceil_div((int64_t)g.clear_bytes, 16 * 256 * 4);
-    stats_gather_kernel<<<blocks + (unsigned)(fill < 4096 ? fill : 4096), 256, 0, st>>>(g, cv, blocks);
+    stats_gather_kernel<<<blocks + transposes + (unsigned)(fill < 4096 ? fill : 4096), 256, 0, st>>>(g, cv, blocks, transposes);
 }
 
 void launch_stats_grad_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const StatsGrad& g, ChunkView cv, hipStream_t st) {
