@@ -15,6 +15,7 @@ __device__ __forceinline__ uint64_t top_key(float z, uint32_t index) {
     const uint32_t o = (b >> 31) ? ~b : b | 0x80000000u;
     return ((uint64_t)(z == z ? o : 1u) << 32) | (uint32_t)~index;
 }
+constexpr uint32_t MINUS_INFINITY = 0x007fffffu;       // high word of -infinity's key
 __device__ __forceinline__ uint32_t top_index(uint64_t key) { return ~(uint32_t)key; }
 __device__ __forceinline__ float top_value(uint64_t key) {
     const uint32_t o = (uint32_t)(key >> 32);
@@ -104,9 +105,10 @@ struct TopList {
         least = last > least ? last : least;
         floor = (uint32_t)(least >> 32) <= 1u ? -__builtin_inff() : top_value(least);
     }
-    // Only keys whose value is at least `key`'s will be wanted: k of those on offer reach it.
+    // Only keys whose value is at least `key`'s will be wanted: k of those on offer reach it. (A bound of -infinity shuts out nothing: it
+    // may be the maximum of a group of NaN.)
     __device__ __forceinline__ void at_least(uint64_t key) {
-        if ((uint32_t)(key >> 32) <= 1u) return;
+        if ((uint32_t)(key >> 32) <= MINUS_INFINITY) return;
         least = (key >> 32 << 32) - 1;
         floor = top_value(key);
     }

@@ -609,3 +609,129 @@ def test_arguments_that_are_refused(P):
         P.dppo_matmul_i8(i.H[:, :64].contiguous(), i.h_scale, i.W[:, :64].contiguous(), i.w_scale)
     with pytest.raises(ValueError):
         P.dppo_matmul_i8(i.H, i.h_scale, i.W, i.w_scale[:-1])
+
+
+@pytest.mark.parametrize("dtype,N,V", [("f32", 3, 20011), ("f32", 90, 600), ("bf16", 3, 9001), ("bf16", 90, 9001), ("bf16", 300, 9001),
+                                       ("bf16", 600, 30001), ("bf16", 4000, 45001), ("i8", 3, 9001), ("i8", 600, 30001)])
+@pytest.mark.parametrize("k", [1, 20, 64])
+def test_a_token_of_nan_only(P, dtype, N, V, k):
+    """A NaN in a token's row of H (in its scale) makes all its logits NaN: distinct alternatives in range all the same, and the other
+    tokens are what they were."""
+    c = Case(dtype, N, 128 if dtype == "i8" else 64, V, seed=30)
+    want = c.call(P, k)
+    at, _ = c.rows()
+    bad = torch.tensor([0, N - 1], device=DEV).unique()
+    if dtype == "i8":
+        c.h_scale[at[bad]] = float("nan")
+    else:
+        c.H[at[bad], 5] = float("nan")
+    out = c.call(P, k)
+    good = torch.ones(N, dtype=torch.bool, device=DEV)
+    good[bad] = False
+    for n in want:
+        assert torch.equal(out[n][good], want[n][good]), n
+    for n in ("logp", "lse", "entropy", "top_logp"):
+        assert torch.isnan(out[n][bad]).all(), n
+    ids = out["top_ids"][bad].long().sort(dim=1).values
+    assert (ids >= 0).all() and (ids < V).all() and (ids.diff(dim=1) > 0).all()
+
+
+@pytest.mark.parametrize("dtype,N", [("f32", 50), ("bf16", 9), ("bf16", 150), ("bf16", 600), ("i8", 9), ("i8", 600)])
+def test_positions_in_any_order_and_more_than_once(P, dtype, N):
+    """The forward pass only reads H: loss positions may repeat, in any order."""
+    c = Case(dtype, N, 128, 3001, seed=31)
+    want = c.call(P, 7)
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    pick = torch.randint(0, N, (N,), generator=gen, device=DEV)
+    c.loss_pos = c.loss_pos[pick].contiguous()
+    out = c.call(P, 7)
+    for n in want:
+        assert torch.equal(out[n], want[n][pick]), n
+
+
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_matmul_i8_of_many_tokens(P, out):
+    """More than 32768 tokens go in chunks; results on odd addresses and lengths, and nothing behind them."""
+    T, D, V = 33001, 128, 77
+    gen = torch.Generator(device=DEV).manual_seed(32)
+    X = torch.randint(-127, 128, (T, D), generator=gen, device=DEV, dtype=torch.int8)
+    W = torch.randint(-127, 128, (V, D), generator=gen, device=DEV, dtype=torch.int8)
+    xs, ws = torch.rand(T, generator=gen, device=DEV) + 0.5, torch.rand(V, generator=gen, device=DEV) + 0.5
+    room = torch.full((T * V + 2,), 7.0, dtype=out, device=DEV)
+    P.dppo_matmul_i8(X, xs, W, ws, out=room[1:-1].view(T, V))
+    acc = (X.double() @ W.double().T).float()
+    assert torch.equal(room[1:-1].view(T, V), (acc * ws * xs[:, None]).to(out))
+    assert room[0] == 7 and room[-1] == 7
+
+
+@pytest.mark.parametrize("dtype,T,N", [("f32", 90, 41), ("bf16", 90, 41), ("bf16", 700, 513), ("i8", 90, 41), ("i8", 700, 513)])
+def test_first_tokens_without_positions(P, dtype, T, N):
+    """loss_pos NULL and N < T: the first N rows, and dH of the others is zero."""
+    import ctypes
+    B = P.binding
+    c = Case(dtype, T, 128, 1001, seed=33, extra=0)
+    want = P.dppo_token_stats(c.H[:N], c.W, c.ids[:N], None, top_k=5, h_scale=None if c.h_scale is None else c.h_scale[:N], w_scale=c.w_scale)
+    code = {"f32": 0, "bf16": 1, "i8": 2}[dtype]
+    shape = B.HeadShape(T, N, c.D, c.V, code)
+    ws = B.alloc_workspace(P.dppo_token_stats_workspace_bytes(T, N, c.D, c.V, code, 5), DEV)
+    got = {n: torch.empty_like(t) for n, t in want.items()}
+    ptr = lambda t: None if t is None else t.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    lib = P.load()
+    assert lib.dppo_token_stats(ctypes.byref(shape), 5, ptr(c.H), ptr(c.W), ptr(c.h_scale), ptr(c.w_scale), ptr(c.ids), None,
+                                *[ptr(got[n]) for n in ("logp", "lse", "entropy", "top_ids", "top_logp")], None, ptr(ws), ws.numel(), stream) == 0
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    if dtype == "i8":
+        return
+    g = [torch.randn(N, device=DEV) for _ in range(3)]
+    ref = P.dppo_token_stats_bwd(c.H[:N], c.W, c.ids[:N], None, want["lse"], want["entropy"], *g)
+    wb = B.alloc_workspace(P.dppo_token_stats_workspace_bytes(T, N, c.D, c.V, code, 0, 1), DEV)
+    dH, dW = torch.full_like(c.H, float("nan")), torch.full(c.W.shape, float("nan"), device=DEV)
+    assert lib.dppo_token_stats_bwd(ctypes.byref(shape), ctypes.byref(B.StatsGradParams(0, 0)), ptr(c.H), ptr(c.W), ptr(c.ids), None,
+                                    ptr(want["lse"]), ptr(want["entropy"]), *[ptr(t) for t in g], ptr(dH), ptr(dW), None, ptr(wb),
+                                    wb.numel(), stream) == 0
+    assert torch.equal(dH[:N], ref["dH"]) and (dH[N:] == 0).all() and torch.equal(dW, ref["dW"])
+
+
+def test_two_calls_at_once(P):
+    """On two streams, each with a workspace of its own."""
+    cases = [Case("bf16", 700, 128, 9001, seed=34), Case("i8", 700, 128, 9001, seed=35)]
+    grads = [make_grads(c, 6, ALL) if c.dtype != "i8" else None for c in cases]
+
+    def both(c, g):
+        f = c.call(P, 9)
+        out = [f[n] for n in ("logp", "lse", "entropy", "top_ids", "top_logp")]
+        if g is not None:
+            out += P.dppo_token_stats_bwd(c.H, c.W, c.ids, c.loss_pos, f["lse"], f["entropy"], dW_dtype=torch.bfloat16, **g).values()
+        return out
+
+    want = [both(c, g) for c, g in zip(cases, grads)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(both(cases[i], grads[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for out in got[i]:
+            for a, b in zip(out, want[i]):
+                assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("N,D,V,out", [(600, 64, 520, torch.float32), (600, 64, 520, torch.bfloat16), (2100, 128, 300, torch.bfloat16),
+                                       (30, 576, 1500, torch.bfloat16), (65, 64, 40000, torch.float32), (1300, 320, 7000, torch.bfloat16)])
+def test_gradient_in_parts(P, N, D, V, out):
+    """Few tiles with a long sum: dH and dW are cut along it. A workspace full of NaN, nothing outside dH and dW is written."""
+    c = Case("bf16", N, D, V, seed=36)
+    g = make_grads(c, 7, ALL)
+    ws = P.binding.alloc_workspace(P.dppo_token_stats_workspace_bytes(c.T, N, D, V, 1, 0, 2 if out == torch.bfloat16 else 1), DEV).fill_(0xFF)
+    pad = 512
+    room_h = torch.full((c.T * D + 2 * pad,), 7.0, dtype=torch.bfloat16, device=DEV)
+    room_w = torch.full((V * D + 2 * pad,), 7.0, dtype=out, device=DEV)
+    r = backward(P, c, g, ws=ws, dH=room_h[pad:-pad].view(c.T, D), dW=room_w[pad:-pad].view(V, D))
+    check_grads(c, g, r)
+    for room in (room_h, room_w):
+        assert (room[:pad] == 7).all() and (room[-pad:] == 7).all()
