@@ -36,15 +36,19 @@ void launch_stats_bf16(const LogitsOut& g, const StatsTiles& t, int cus, hipStre
 }
 
 int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups) {
+    static_assert(CfgBig::GROUP_M == CfgBig192::GROUP_M && CfgBig::BM == CfgBig192::BM, "the same bands");
     *groups = 0;
-    if (top_k == 0 || tile != TILE_256x256) return 0;
-    const int tiles_m = (int)ceil_div(V, CfgBig::BM), tiles_n = (int)ceil_div(n, CfgBig::BN), tiles = tiles_m * tiles_n;
-    const int bands = tiles_m / CfgBig::GROUP_M, band = CfgBig::GROUP_M * tiles_n;
-    int lead = tiles_m / LEAD_SHARE / CfgBig::GROUP_M;
-    // to the nearest whole rounds of the chip
-    const int rounds = (lead * band + cus / 2) / cus;
-    if (rounds > 0) lead = (rounds * cus + band / 2) / band;
-    if (lead >= bands || lead * CfgBig::GROUP_M * STATS_GROUPS < 2 * top_k) return 0;
+    if (top_k == 0 || (tile != TILE_256x256 && tile != TILE_256x192)) return 0;
+    const int tiles_m = (int)ceil_div(V, CfgBig::BM), tiles_n = (int)ceil_div(n, tile == TILE_256x256 ? CfgBig::BN : CfgBig192::BN);
+    const int tiles = tiles_m * tiles_n, bands = tiles_m / CfgBig::GROUP_M, band = CfgBig::GROUP_M * tiles_n;
+    // twice top_k groups at least (of as many as top_k, the last one's maximum is a bound of little use)
+    const int share = tiles_m / LEAD_SHARE / CfgBig::GROUP_M, least = (int)ceil_div(2 * top_k, CfgBig::GROUP_M * STATS_GROUPS);
+    int lead = share > least ? share : least;
+    // to the nearest whole rounds of the chip, up where the nearest are too few
+    int rounds = (lead * band + cus / 2) / cus;
+    if ((rounds * cus + band / 2) / band < least) ++rounds;
+    lead = (rounds * cus + band / 2) / band;
+    if (2 * lead > bands || lead < least) return 0;
     // a launch more may cost a round more: few rounds are only cut where it does not
     auto in_rounds = [&](int t) { return (t + cus - 1) / cus; };
     if (in_rounds(tiles) < LEAD_ROUNDS && in_rounds(lead * band) + in_rounds(tiles - lead * band) > in_rounds(tiles)) return 0;

@@ -94,21 +94,26 @@ inline int32_t tile_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : t
 // Rows of a group of a tile (see StatsPart).
 inline int32_t group_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile_rows(tile) / STATS_GROUPS; }
 // For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
-// kernel for few tokens hold. Up to 192 tokens as for the log-probabilities alone (see CfgFew). Beyond, tiles of 128 x 128, two per
-// compute unit, while large ones would fill no more than half the chip, or a second round of it less than a quarter.
-// Statistics of D = 512, 128 x 128 / 256 x 256: V = 4000, 500 tokens (32 large tiles) 9 / 17 us, 2000 (128) 13 / 18, 4000 (256) 24 / 21;
-// V = 40000, 500 tokens (314) 30 / 36; of D = 2560: 24 / 47, 42 / 53, 98 / 65; 98 / 112; 1000 tokens (628) 188 / 175.
+// kernel for few tokens hold. Up to 128 tokens as for the log-probabilities alone (see CfgFew). Beyond, the tile whose rounds of the chip
+// take the least time, 256 x 256 : 256 x 192 : two of 128 x 128 as 20 : 18 : 15, the last while large tiles fill no more than two rounds.
+// Statistics, 256 x 256 / 256 x 192 / 128 x 128, with the rounds of each: D = 1024, V = 32000: 224 tokens (1/1/1) 30 / 29 / 22 us, 384
+// (1/1/2) 34 / 29 / 34, 512 (1/2/2) 35 / 44 / 37, 576 (2/2/3) 54 / 44 / 48, 768 (2/2/3) 55 / 48 / 52, 1024 (2/3/4) 61 / 72 / 72, 1152
+// (3/3/5) 82 / 70 / 80; D = 4096, V = 60000: 224 (1/2/2) 144 / 163 / 157, 576 (3/3/5) 255 / 233 / 294, 1152 (5/6/9) 430 / 435 / 523;
+// D = 2560, V = 151936: 192 (3/3/10) 216 / 201 / 244, 384 (5/5/14) 297 / 287 / 335, 640 (7/10/-) 423 / 496 / 530.
+constexpr int64_t SMALL_TILES_MOST = 512;
 inline int logits_tile(int32_t n, int32_t V, int32_t k2, bool i8) {
     if (n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16)) return TILE_FEW;
     if (n <= 96) return TILE_128x96;
     if (n <= 128) return TILE_128x128;
     constexpr int64_t CHIP = 256;                 // compute units
-    const int64_t large = ceil_div(V, 256) * ceil_div(n, 256);
-    if (2 * large <= CHIP || (large > CHIP && 4 * large <= 5 * CHIP)) return TILE_128x128;
-    return n <= 192 ? TILE_256x192 : TILE_256x256;
+    const int64_t rows = ceil_div(V, 256), large = rows * ceil_div(n, 256);
+    const int64_t t256 = 20 * ceil_div(large, CHIP), t192 = 18 * ceil_div(rows * ceil_div(n, 192), CHIP);
+    const int64_t t128 = 15 * ceil_div(ceil_div(V, 128) * ceil_div(n, 128), 2 * CHIP);
+    if (large <= SMALL_TILES_MOST && t128 < t256 && t128 < t192) return TILE_128x128;
+    return t192 < t256 ? TILE_256x192 : TILE_256x256;
 }
-// Most pairs of (tile, token) that 128 x 128 tiles beyond 128 tokens make: 5/4 of a chip of large tiles.
-constexpr size_t SMALL_TILE_PAIRS = 2 * 320 * 256;
+// Most pairs of (tile, token) that 128 x 128 tiles beyond 128 tokens make.
+constexpr size_t SMALL_TILE_PAIRS = 2 * SMALL_TILES_MOST * 256;
 // Logits of n tokens, C[n, V] = H W^T with pitch ldc, by tiles of the given kind. k2: bytes of an operand row / 2 (a multiple of 64). Row n
 // of the tokens is row map[n] (clamped to h_rows) of H, or n where map is NULL, as it has to be for the largest tile.
 struct LogitsOut {
@@ -121,7 +126,7 @@ struct LogitsOut {
 // tau: of groups whose maximum does not exceed tau[n] the logits are not stored (NULL: all are). first, count: tiles of the launch in the
 // order of the walk (count < 0: to the last).
 struct StatsTiles { StatsPart part; TokenArgs tokens; const int32_t* y; ChunkView cv; const float* tau; int first, count; };
-// Leading tiles of the walk, whole bands of rows from vocabulary entry 0 on, that a call with alternatives launches ahead of the rest
+// Leading tiles of the walk (256 rows), whole bands of rows from vocabulary entry 0 on, that a call with alternatives launches ahead of the rest
 // (0: none), and how many groups of rows they are.
 int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int32_t* groups);
 int mfma_stats_setup(int* compute_units);
