@@ -201,10 +201,7 @@ struct FewStats : FewScales<I8> {
     }
     __device__ __forceinline__ void finish(const State& state, int u, int n, int lane) const {
         // a token's rows are in four lanes
-        Stats s = state.s;
-#pragma unroll
-        for (int off = MB; off < 64; off *= 2)
-            s = join(s, Stats{__shfl_xor(s.m, off, 64), __shfl_xor(s.sum, off, 64), __shfl_xor(s.dev, off, 64)});
+        const Stats s = join_lanes<MB>(state.s);
         if (lane < n) {                          // (lanes 0 to 15 hold the tokens)
             part.mx[(size_t)u * part.pitch + lane] = s.m;
             part.sd[(size_t)u * part.pitch + lane] = make_float2(s.sum, s.dev);

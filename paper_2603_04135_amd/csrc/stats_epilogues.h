@@ -198,8 +198,7 @@ struct EpiStats : OperandTag<I8> {
                         if (!FULL && c.m0 + mi * MB + acc_row(c.lane, j) >= c.M) z[mi][ni][j] = NEG_INF;
                         m = fmaxf(m, z[mi][ni][j]);
                     }
-                m = fmaxf(m, __shfl_xor(m, 16, 64));
-                m = fmaxf(m, __shfl_xor(m, 32, 64));
+                m = pair_max<32>(pair_max<16>(m));
                 const int n = c.n0 + ni * MB + acc_col(c.lane);
                 if (STORE) {
                     // whole groups, the padding of the vocabulary too (the pitch holds it)
@@ -220,10 +219,8 @@ struct EpiStats : OperandTag<I8> {
                         sum += e;
                         dev = fmaf(fmaxf(d, DEV_MIN), e, dev);
                     }
-                sum += __shfl_xor(sum, 16, 64);
-                sum += __shfl_xor(sum, 32, 64);
-                dev += __shfl_xor(dev, 16, 64);
-                dev += __shfl_xor(dev, 32, 64);
+                sum = pair_sum<32>(pair_sum<16>(sum));
+                dev = pair_sum<32>(pair_sum<16>(dev));
                 if (c.lane < MB && n < n_c) {
                     part.mx[g + n] = m;
                     part.sd[g + n] = make_float2(sum, dev);

@@ -1,6 +1,7 @@
 // Internal declarations of the token statistics, their gradient and the 8-bit operators.
 #pragma once
 #include "dppo_internal.h"
+#include "lanes.h"
 
 namespace dppo {
 
@@ -24,6 +25,13 @@ __device__ __forceinline__ Stats join(const Stats& a, const Stats& b) {
     const float da = a.m - ref, db = b.m - ref, ea = exp_fast(da), eb = exp_fast(db);
     return Stats{m, a.sum * ea + b.sum * eb,
                  ea * (a.dev + fmaxf(da, DEV_MIN) * a.sum) + eb * (b.dev + fmaxf(db, DEV_MIN) * b.sum)};
+}
+// Over the lanes whose numbers differ in bit FROM and above.
+template <int FROM>
+__device__ __forceinline__ Stats join_lanes(Stats s) {
+    s = join(s, Stats{xor_lane<FROM>(s.m), xor_lane<FROM>(s.sum), xor_lane<FROM>(s.dev)});
+    if constexpr (FROM < 32) s = join_lanes<2 * FROM>(s);
+    return s;
 }
 // Rows of logits cut into parts: per (token, part) the statistics {max, sum, dev, -} and the top_k keys.
 struct PartialStats {

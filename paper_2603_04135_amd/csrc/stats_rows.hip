@@ -10,12 +10,6 @@
 namespace dppo {
 namespace {
 
-__device__ __forceinline__ Stats join_lanes(Stats s) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1)
-        s = join(s, Stats{__shfl_xor(s.m, off, 64), __shfl_xor(s.sum, off, 64), __shfl_xor(s.dev, off, 64)});
-    return s;
-}
 
 // What one token's statistics and alternatives go to (any of the pointers may be NULL).
 __device__ __forceinline__ void write_token(const StatsOut& o, int64_t n, const Stats& s, float target_logit) {
@@ -54,14 +48,14 @@ template <bool TOP>
 __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* __restrict__ Z, int64_t ldz, TokenArgs a, StatsOut o,
                                                                   ChunkView cv, PartialStats partial) {
     __shared__ Stats red[ROWS_WAVES];
-    __shared__ uint64_t lists[ROWS_WAVES][TOP_MAX];
+    __shared__ uint64_t lists[TOP ? ROWS_WAVES : 1][PENDING4];
     const int n = blockIdx.x, part = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const float NONE = -__builtin_inff();
     const float* z = Z + (size_t)n * ldz;
     const int vectors = (a.V + 3) / 4;
     const int lo = (int)((int64_t)vectors * part / partial.parts), hi = (int)((int64_t)vectors * (part + 1) / partial.parts);
     Stats s = no_stats();
-    TopList top(lists[wave]);
+    TopList top(lists[TOP ? wave : 0]);
     // (whole wavefronts walk the loop: the list needs every lane)
     for (int i0 = lo + wave * 64; i0 < hi; i0 += ROWS_THREADS * ROWS_UNROLL) {
         float x[ROWS_UNROLL][4], m4[ROWS_UNROLL];
@@ -92,17 +86,17 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
             }
         s = join(s, b);
         if (TOP) {
+            // (k lanes' maxima of the first logits bound what the list begins with)
+            if (i0 == lo + wave * 64) top.at_least(kth_of_lanes(m, o.top_k, lane));
 #pragma unroll
             for (int u = 0; u < ROWS_UNROLL; ++u) {
                 if (!__any(!(m4[u] < top.floor))) continue;
                 const int i = i0 + u * ROWS_THREADS + lane;
-#pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    top.offer(i < hi && i * 4 + q < a.V ? top_key(x[u][q], (uint32_t)(i * 4 + q)) : 0, o.top_k, lane);
+                top.offer4(x[u], i * 4, i < hi ? a.V : 0, o.top_k, lane);
             }
         }
     }
-    s = join_lanes(s);
+    s = join_lanes<1>(s);
     if (lane == 0) red[wave] = s;
     if (TOP) {
         top.flush(o.top_k, lane);
@@ -144,8 +138,8 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
         const float4 v = partial.stats[at + p];
         s = join(s, Stats{v.x, v.y, v.z});
     }
-    s = join_lanes(s);
-    __shared__ uint64_t pending[TOP_MAX];
+    s = join_lanes<1>(s);
+    __shared__ uint64_t pending[PENDING];
     TopList top(pending);
     if (TOP) {
         const int entries = partial.parts * o.top_k;
@@ -169,17 +163,18 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
 // token lie in the k groups with the largest maxima (in the order of maximum, then group: every group ahead of another one holds a
 // logit that is ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
 // The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
-// list the groups, and the first of them their logits.
+// list the groups, and after that their logits. (Bound by latency up to some 2000 tokens.)
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 6;
 template <int TOK, bool TOP>
 __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t rows, const float* __restrict__ Z, int64_t ldz,
                                                                   TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
     constexpr int LANES = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;       // lanes and wavefronts per token
     constexpr int ROW = TOK + 1, BLOCK = JOIN_MAXIMA / TOK;                 // maxima in LDS: row pitch, groups of a block
-    __shared__ float maxima[TOP ? BLOCK * ROW : 1];
+    __shared__ __attribute__((aligned(8))) float maxima[TOP ? BLOCK * ROW : 1];      // and then the logits that wait for a list
+    static_assert(BLOCK * ROW * 4 >= JOIN_WAVES * PENDING4 * 8, "LDS");
     __shared__ Stats red[JOIN_WAVES][TOK];
     __shared__ Stats fin[TOK];
-    __shared__ uint64_t lists[TOP ? JOIN_WAVES : 1][TOP_MAX];               // of the wavefronts: newcomers, then lists that are shared
+    __shared__ uint64_t lists[TOP ? JOIN_WAVES : 1][PENDING];               // of the wavefronts: groups that wait, then lists that are shared
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int tok = tid % TOK, n = blockIdx.x * TOK + tok;
     const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
@@ -225,70 +220,80 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
             if (b1 == groups) top.flush(o.top_k, lane);
         }
     }
-#pragma unroll
-    for (int off = TOK; off < 64; off <<= 1)
-        s = join(s, Stats{__shfl_xor(s.m, off, 64), __shfl_xor(s.sum, off, 64), __shfl_xor(s.dev, off, 64)});
+    s = join_lanes<TOK>(s);
     if (lane < TOK) red[wave][lane] = s;
     __syncthreads();
-    if (tid < TOK) {
-        for (int w = 1; w < JOIN_WAVES; ++w) s = join(s, red[w][tid]);
-        if (TOP) fin[tid] = s;
-        if (n < cv.n_c) {
-            const int64_t gi = cv.n0 + n;
-            if (look_up && a.status != nullptr) report_token(a, gi);
-            write_token(o, gi, s, part.zy ? part.zy[n] : 0.0f);
+    if (wave == 0) {
+        s = no_stats();
+        for (int w = lane / TOK; w < JOIN_WAVES; w += 64 / TOK) s = join(s, red[w][tok]);
+        s = join_lanes<TOK>(s);
+        if (lane < TOK) {
+            if (TOP) fin[tok] = s;
+            if (n < cv.n_c) {
+                const int64_t gi = cv.n0 + n;
+                if (look_up && a.status != nullptr) report_token(a, gi);
+                write_token(o, gi, s, part.zy ? part.zy[n] : 0.0f);
+            }
         }
     }
     if (!TOP) return;
-    __syncthreads();
-    // the token's first wavefront ends with its list
-    if (WPT > 1) {
+    // the token's first wavefront ends with all of its lists joined
+    auto join_lists = [&](TopList& list) __attribute__((always_inline)) {
 #pragma unroll
         for (int d = 1; d < WPT; d *= 2) {
             if (d > 1) __syncthreads();
-            if (sub % (2 * d) == d) lists[wave][lane] = top.entry;
+            if (sub % (2 * d) == d) lists[wave][lane] = list.entry;
             __syncthreads();
-            if (sub % (2 * d) == 0) top.merge(lists[wave + d][lane], lane);
+            if (sub % (2 * d) == 0) list.merge(lists[wave + d][lane], lane);
         }
-    }
-    if (sub != 0 || my_n >= cv.n_c) return;
-    // ... and reads the groups' logits: all loads of 8 rounds under way at once, one round a lane's float4
+    };
+    join_lists(top);
+    if (sub == 0) lists[wave][lane] = top.entry;
+    __syncthreads();
+    const uint64_t group = lists[wave - sub][lane];
+    // all of them read the groups' logits: all loads of 8 rounds under way at once, one round a lane's float4, rows / 4 lanes a group. (One
+    // round at a time is looked at by code that is there once: unrolled, it does not fit the instruction cache.)
     constexpr int ROUNDS = 8;
-    TopList best(lists[wave]);
-    const int count = groups < o.top_k ? groups : o.top_k;
-    // the k-th largest maximum: k logits are no smaller
-    if (count == o.top_k) best.at_least(lane_value(top.entry, count - 1));
-    const float* z = Z + (size_t)my_n * ldz;
-    // rows / 4 lanes read a group
-    const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
-    for (int i0 = 0; i0 < count; i0 += per * ROUNDS) {
-        float4 x[ROUNDS];
-        int v0[ROUNDS];
+    TopList best(reinterpret_cast<uint64_t*>(maxima) + wave * PENDING4);
+    if (my_n < cv.n_c) {
+        const int count = groups < o.top_k ? groups : o.top_k;
+        // the k-th largest maximum: k logits are no smaller
+        if (count == o.top_k) best.at_least(lane_value(group, count - 1));
+        const float* z = Z + (size_t)my_n * ldz;
+        const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
+        for (int i0 = sub * per; i0 < count; i0 += per * WPT * ROUNDS) {
+            float x[ROUNDS][4];
+            int v0[ROUNDS];
 #pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            const int i = i0 + u * per + which;
-            const uint32_t g = ~(uint32_t)__shfl((int)(uint32_t)top.entry, i < count ? i : 0, 64);
-            v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
-            if (v0[u] < a.V) x[u] = *reinterpret_cast<const float4*>(z + v0[u]);
+            for (int u = 0; u < ROUNDS; ++u) {
+                const int i = i0 + u * per * WPT + which;
+                const uint32_t g = top_index((uint64_t)(uint32_t)__shfl((int)(uint32_t)group, i < count ? i : 0, 64));
+                v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
+                if (v0[u] < a.V) *reinterpret_cast<float4*>(x[u]) = *reinterpret_cast<const float4*>(z + v0[u]);
+            }
+#pragma unroll 1
+            for (int i = i0; i < count && i < i0 + per * WPT * ROUNDS; i += per * WPT) {
+                const float m = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
+                if (__any(v0[0] < a.V && !(m < best.floor))) best.offer4(x[0], v0[0], a.V, o.top_k, lane);
+#pragma unroll
+                for (int u = 0; u + 1 < ROUNDS; ++u) {
+                    v0[u] = v0[u + 1];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) x[u][q] = x[u + 1][q];
+                }
+            }
         }
-#pragma unroll
-        for (int u = 0; u < ROUNDS; ++u) {
-            if (i0 + u * per >= count) break;
-            const float xx[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                best.offer(v0[u] + q < a.V ? top_key(xx[q], (uint32_t)(v0[u] + q)) : 0, o.top_k, lane);
-        }
+        best.flush(o.top_k, lane);
     }
-    best.flush(o.top_k, lane);
-    write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
+    join_lists(best);
+    if (sub == 0 && my_n < cv.n_c) write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
 }
 
 // tau[n]: one wavefront per token lists the maxima of the leading groups, read with neighbouring tokens side by side.
 constexpr int BOUND_TOK = 16, BOUND_BLOCK = 640;
 __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32_t groups, int32_t top_k, int32_t n_c, float* __restrict__ tau) {
     __shared__ float maxima[BOUND_BLOCK * (BOUND_TOK + 1)];
-    __shared__ uint64_t pending[16][TOP_MAX];
+    __shared__ uint64_t pending[16][PENDING];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int tok = tid % BOUND_TOK, n = blockIdx.x * BOUND_TOK + tok, my_n = blockIdx.x * BOUND_TOK + wave;
     TopList top(pending[wave]);

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "lanes.h"
+
 namespace dppo {
 
 constexpr int TOP_MAX = 64;     // one entry per lane
@@ -27,17 +29,6 @@ __device__ __forceinline__ uint64_t lane_value(uint64_t v, int lane) {
     return ((uint64_t)hi << 32) | lo;
 }
 
-// The value of lane (own lane ^ X): by data-parallel primitives where one says it, else through the LDS crossbar.
-template <int X>
-__device__ __forceinline__ uint32_t xor_lane(uint32_t v) {
-    constexpr int ctrl = X == 1 ? 0xB1 : X == 2 ? 0x4E : X == 3 ? 0x1B : X == 7 ? 0x141 : X == 8 ? 0x128 : X == 15 ? 0x140 : 0;
-    if constexpr (ctrl != 0) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, 0xf, 0xf, true);
-    else return (uint32_t)__shfl_xor((int)v, X, 64);
-}
-template <int X>
-__device__ __forceinline__ uint64_t xor_lane(uint64_t v) {
-    return ((uint64_t)xor_lane<X>((uint32_t)(v >> 32)) << 32) | xor_lane<X>((uint32_t)v);
-}
 // Of a pair of lanes X apart, the one with the lower number (bit BIT clear) keeps the larger key.
 template <int X, int BIT>
 __device__ __forceinline__ uint64_t exchange(uint64_t v, int lane) {
@@ -65,8 +56,9 @@ __device__ __forceinline__ uint64_t kth_of_lanes(float z, int k, int lane) {
     return lane_value(sort_lanes(top_key(z, 0) >> 32, lane), k - 1) << 32;
 }
 
-// Newcomers that beat the list's last entry gather in LDS (`pending`, 64 keys of this wavefront) and are sorted and merged when there
-// are 64 of them, or at the end: some 10 instructions for 64 on offer and 300 a merge, against 20 for each that is inserted by itself.
+// Newcomers that beat the list's last entry gather in LDS (`pending`, of this wavefront) and are sorted and merged by 64, and what is left at
+// the end: some 10 instructions for 64 on offer and 250 a merge, against 20 for each that is inserted by itself.
+constexpr int PENDING = 128, PENDING4 = 320;     // keys of a buffer for lists that are offered one key a lane at a time, or four
 struct TopList {
     uint64_t* pending;
     int waiting = 0;
@@ -75,26 +67,39 @@ struct TopList {
     float floor = -__builtin_inff();   // the same as a logit: a lower one need not be looked at (-infinity while there are not k)
 
     __device__ __forceinline__ explicit TopList(uint64_t* lds) : pending(lds) {}
-    // All lanes: lane l's key joins the list if it exceeds `least`.
-    __device__ __forceinline__ void offer(uint64_t key, int k, int lane) {
+    // All lanes: lane l's key waits if it exceeds `least`.
+    __device__ __forceinline__ void add(uint64_t key) {
         const bool hit = key > least;
         const uint64_t hits = __ballot(hit);
         if (hits == 0) return;
-        const int count = __builtin_popcountll(hits);
-        if (waiting + count > 64) flush(k, lane);
         if (hit) pending[waiting + __builtin_amdgcn_mbcnt_hi((uint32_t)(hits >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)hits, 0))] = key;
-        waiting += count;
+        waiting += __builtin_popcountll(hits);
     }
-    __device__ __forceinline__ void flush(int k, int lane) {
-        if (waiting == 0) return;
-        // (the wavefront's own LDS accesses stay in order; the compiler has to leave them so)
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const uint64_t key = lane < waiting ? pending[lane] : 0;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        merge(sort_lanes(key, lane), lane);
-        waiting = 0;
-        settle(k);
+    // Takes in those that wait, 64 at a time, until no more than `keep` are left.
+    __device__ __forceinline__ void take(int k, int lane, int keep) {
+#pragma unroll 1
+        while (waiting > keep) {
+            const int n = waiting < 64 ? waiting : 64;
+            waiting -= n;
+            // (the wavefront's own LDS accesses stay in order; the compiler has to leave them so)
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            const uint64_t key = lane < n ? pending[waiting + lane] : 0;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            merge(sort_lanes(key, lane), lane);
+            settle(k);
+        }
     }
+    __device__ __forceinline__ void offer(uint64_t key, int k, int lane) {
+        add(key);
+        take(k, lane, 63);
+    }
+    // The lane's logits x[0 .. 3] of indices v to v + 3, those below V.
+    __device__ __forceinline__ void offer4(const float (&x)[4], int v, int V, int k, int lane) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) add(v + q < V ? top_key(x[q], (uint32_t)(v + q)) : 0);
+        take(k, lane, 63);
+    }
+    __device__ __forceinline__ void flush(int k, int lane) { take(k, lane, 0); }
     // Joins keys in descending order: the larger of each mirrored pair are the 64 largest, in bitonic order.
     __device__ __forceinline__ void merge(uint64_t sorted, int lane) {
         const uint64_t o = xor_lane<63>(sorted);
