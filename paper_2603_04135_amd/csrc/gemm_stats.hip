@@ -6,10 +6,11 @@ namespace dppo {
 namespace {
 
 DeviceSetup g_setup;
-// Of the logits of a call with alternatives, an eighth of the vocabulary is stored whole, and of the rest what exceeds the bound found
-// there (some 15 % of the groups with 20 alternatives of 151936). 8191 tokens of D = 2560, GEMM and bound, lead of a quarter / an eighth /
-// a sixteenth / none 4545 / 4555 / 4618 / 4982 us (4435 without alternatives), 3000 tokens 1754 / 1731 / 1760 / -, 300 355 / 354 / 400 / 377.
-constexpr int LEAD_SHARE = 8, LEAD_ROUNDS = 10;
+// Of the logits of a call with alternatives, those of leading tiles are stored whole, and of the rest what exceeds the bound found there (see
+// stats_lead_tiles): 12 % and some 13 % with 20 alternatives of 151936. 8191 tokens of D = 2560, GEMM and bound, lead of a quarter / an
+// eighth / a sixteenth / none 4545 / 4555 / 4618 / 4982 us (4435 without alternatives), 3000 tokens 1754 / 1731 / 1760 / -, 300 355 / 354
+// / 400 / 377.
+constexpr int LEAD_ROUNDS = 10;
 typedef EpiStore<2> EpiStoreDW16;
 // Gradient entries of up to 64 tokens, or where large tiles fill at most half the chip, by tiles of 64 tokens. D = 1152, 64 / 256 tokens a
 // tile: 2 tokens, V = 20000 13 / 28 us; 1016, V = 1516 (24 large tiles) 14 / 32, V = 6000 (96) 27 / 32; 300, V = 15160 (120) 26 / 31;
@@ -41,13 +42,15 @@ int stats_lead_tiles(int tile, int32_t V, int32_t n, int32_t top_k, int cus, int
     if (top_k == 0 || (tile != TILE_256x256 && tile != TILE_256x192)) return 0;
     const int tiles_m = (int)ceil_div(V, CfgBig::BM), tiles_n = (int)ceil_div(n, tile == TILE_256x256 ? CfgBig::BN : CfgBig192::BN);
     const int tiles = tiles_m * tiles_n, bands = tiles_m / CfgBig::GROUP_M, band = CfgBig::GROUP_M * tiles_n;
-    // twice top_k groups at least (of as many as top_k, the last one's maximum is a bound of little use)
-    const int share = tiles_m / LEAD_SHARE / CfgBig::GROUP_M, least = (int)ceil_div(2 * top_k, CfgBig::GROUP_M * STATS_GROUPS);
-    int lead = share > least ? share : least;
-    // to the nearest whole rounds of the chip, up where the nearest are too few
+    // L leading groups of all G are stored whole, and of the others those that are among a token's top_k of L + 1: a share of top_k / L.
+    // L = sqrt(top_k G) stores the least.
+    const double all = (double)tiles_m * STATS_GROUPS, best = sqrt(top_k * all);
+    const int least = (int)ceil_div(2 * top_k, CfgBig::GROUP_M * STATS_GROUPS);
+    int lead = (int)(best / (CfgBig::GROUP_M * STATS_GROUPS) + 0.5);
+    // what fits the nearest number of rounds of the chip, one more where that is too little
     int rounds = (lead * band + cus / 2) / cus;
-    if ((rounds * cus + band / 2) / band < least) ++rounds;
-    lead = (rounds * cus + band / 2) / band;
+    if (rounds * cus / band < least) ++rounds;
+    lead = rounds * cus / band;
     if (2 * lead > bands || lead < least) return 0;
     // a launch more may cost a round more: few rounds are only cut where it does not
     auto in_rounds = [&](int t) { return (t + cus - 1) / cus; };
