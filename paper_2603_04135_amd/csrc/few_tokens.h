@@ -203,8 +203,8 @@ struct FewStats : FewScales<I8> {
         // a token's rows are in four lanes
         const Stats s = join_lanes<MB>(state.s);
         if (lane < n) {                          // (lanes 0 to 15 hold the tokens)
-            part.mx[(size_t)u * part.pitch + lane] = s.m;
-            part.sd[(size_t)u * part.pitch + lane] = make_float2(s.sum, s.dev);
+            part.mx[part.at(u, lane)] = s.m;
+            part.sd[part.at(u, lane)] = make_float2(s.sum, s.dev);
         }
     }
 };

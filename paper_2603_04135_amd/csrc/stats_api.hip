@@ -215,8 +215,9 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
             if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
         }
+        const bool alone = cv.n_c <= JOIN_ALONE;
         StatsTiles t{{reinterpret_cast<float*>(w + r.o_mx), reinterpret_cast<float2*>(w + r.o_sd),
-                      logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, gather ? cv.n_cp : cv.n_c},
+                      logp ? reinterpret_cast<float*>(w + r.o_zy) : nullptr, alone ? 1 : cv.n_c, alone ? groups_of_tiles(tile, s.V) : 1},
                      tokens, gather ? y : nullptr, cv, nullptr, 0, -1};
         auto gemm = [&]() {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);

@@ -185,7 +185,7 @@ struct EpiStats : OperandTag<I8> {
         f32x4 z[MI][NI];
         to_logits<Cfg>(acc, z, pre.scales);
         static_assert(Cfg::WGM == STATS_GROUPS, "a wavefront's rows = a group");
-        const size_t g = (size_t)(c.tm * STATS_GROUPS + c.wave_m) * part.pitch;
+        const int g = c.tm * STATS_GROUPS + c.wave_m;
         auto reduce = [&](auto full_tag) __attribute__((always_inline)) {
             constexpr bool FULL = decltype(full_tag)::value;
 #pragma unroll
@@ -222,8 +222,8 @@ struct EpiStats : OperandTag<I8> {
                 sum = pair_sum<32>(pair_sum<16>(sum));
                 dev = pair_sum<32>(pair_sum<16>(dev));
                 if (c.lane < MB && n < n_c) {
-                    part.mx[g + n] = m;
-                    part.sd[g + n] = make_float2(sum, dev);
+                    part.mx[part.at(g, n)] = m;
+                    part.sd[part.at(g, n)] = make_float2(sum, dev);
                 }
             }
         };

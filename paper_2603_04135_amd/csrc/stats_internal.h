@@ -41,10 +41,14 @@ struct PartialStats {
 int stats_row_parts(int32_t n_c, int32_t V, int cus);
 void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const StatsOut& o, ChunkView cv, PartialStats partial, hipStream_t st);
 
-// Statistics of the vocabulary GEMM by groups of rows, STATS_GROUPS of a tile (a unit of the kernel for few tokens is one): mx[g * pitch + n]
-// is group g's maximum for token n, sd[g * pitch + n] = {sum, dev} against it; zy[n]: target logits (or NULL).
-constexpr int STATS_GROUPS = 2;
-struct StatsPart { float* mx; float2* sd; float* zy; int32_t pitch; };
+// Statistics of the vocabulary GEMM by groups of rows, STATS_GROUPS of a tile (a unit of the kernel for few tokens is one): mx[at(g, n)]
+// is group g's maximum for token n, sd[at(g, n)] = {sum, dev} against it; zy[n]: target logits (or NULL). A token's groups lie side by side
+// up to JOIN_ALONE tokens, which a workgroup each joins, beyond that the tokens of a group.
+constexpr int STATS_GROUPS = 2, JOIN_ALONE = 256;
+struct StatsPart {
+    float* mx; float2* sd; float* zy; int32_t group_step, token_step;
+    __device__ __forceinline__ size_t at(int g, int n) const { return (size_t)g * group_step + (size_t)n * token_step; }
+};
 // Joins a token's groups (of `rows` rows) and picks the top alternatives from the stored logits of the groups that can hold them.
 void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t ldz, const TokenArgs& a, bool look_up,
                        const StatsOut& o, ChunkView cv, hipStream_t st);
@@ -101,6 +105,8 @@ constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 =
 inline int32_t tile_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile <= TILE_128x128 ? 128 : 256; }
 // Rows of a group of a tile (see StatsPart).
 inline int32_t group_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile_rows(tile) / STATS_GROUPS; }
+// Groups of all tiles (the last may lie behind the vocabulary).
+inline int32_t groups_of_tiles(int tile, int32_t V) { return (int32_t)ceil_div(V, tile_rows(tile)) * (tile == TILE_FEW ? 1 : STATS_GROUPS); }
 // For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
 // kernel for few tokens hold. Up to 128 tokens as for the log-probabilities alone (see CfgFew). Beyond, the tile whose rounds of the chip
 // take the least time, 256 x 256 : 256 x 192 : two of 128 x 128 as 20 : 18 : 15, the last while large tiles fill no more than two rounds.

@@ -192,8 +192,8 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
                     const int g = g0 + u * LANES;
                     if (g >= b1) break;
-                    m[u] = part.mx[(size_t)g * part.pitch + n];
-                    sd[u] = part.sd[(size_t)g * part.pitch + n];
+                    m[u] = part.mx[part.at(g, n)];
+                    sd[u] = part.sd[part.at(g, n)];
                 }
 #pragma unroll
                 for (int u = 0; u < JOIN_UNROLL; ++u) {
@@ -301,7 +301,7 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
         const int g1 = groups - g0 < BOUND_BLOCK ? groups : g0 + BOUND_BLOCK;
         if (g0 > 0) __syncthreads();
         if (n < n_c) {
-            for (int g = g0 + tid / BOUND_TOK; g < g1; g += 1024 / BOUND_TOK) maxima[(g - g0) * (BOUND_TOK + 1) + tok] = part.mx[(size_t)g * part.pitch + n];
+            for (int g = g0 + tid / BOUND_TOK; g < g1; g += 1024 / BOUND_TOK) maxima[(g - g0) * (BOUND_TOK + 1) + tok] = part.mx[part.at(g, n)];
         }
         __syncthreads();
         for (int i = g0; i < g1; i += 64)
@@ -469,9 +469,9 @@ void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t 
         if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
         else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
     };
-    // As many tokens a workgroup as leave every compute unit at most one, from 4 on; one where there are few tokens with many groups. V = 151936,
-    // 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 25.6 / 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83.
-    if (cv.n_c <= FEW_TILE_TOKENS) go(std::integral_constant<int, 1>{});
+    // As many tokens a workgroup as leave every compute unit at most one. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 25.6 /
+    // 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83.
+    if (cv.n_c <= JOIN_ALONE) go(std::integral_constant<int, 1>{});
     else if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
     else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});
     else go(std::integral_constant<int, 16>{});
