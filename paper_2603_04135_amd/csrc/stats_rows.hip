@@ -470,7 +470,7 @@ void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t 
         else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
     };
     // As many tokens a workgroup as leave every compute unit at most one. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 25.6 /
-    // 23.9 / 31.0 us, 2000 51 / 29 / 33, 8000 189 / 119 / 83.
+    // 22.0 / 26.4 us, 2000 51 / 29 / 28, 8000 199 / 120 / 84.
     if (cv.n_c <= JOIN_ALONE) go(std::integral_constant<int, 1>{});
     else if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
     else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});
