@@ -206,19 +206,16 @@ int launch_mfma_logits_grad(const void* W, int32_t V, int32_t D, const void* Hc,
 // dH rows of a chunk: C[n_c, D] = diag(row_scale) G[n_c, Vp] W[V, D] with G in the blocked chunk layout (pitch Vp)
 // and W read from WT, its transpose in the blocked B-operand layout, or as it lies if WT is NULL; row_scale may be NULL (= 1). `partial` (or NULL): scratch of
 // partial_floats floats, at least mfma_dw_partial_bytes() bytes, for the partial tiles of a last round that is cut along K.
-// k_parts > 0: all tiles, fewer than compute units, are cut into so many parts along K; 0: as many as pay for a long K.
 void launch_mfma_dh(int cus, const void* G, int32_t Vp, const void* WT, const void* W, int32_t V, int32_t n_c, int32_t D,
-                    const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st, int k_parts = 0);
-// Tiles of the dH GEMM.
-int mfma_dh_tiles(int32_t n_c, int32_t D);
+                    const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st);
 // dW of a chunk: C[V, D] (+)= G^T HcT^T = sum_n G[n, v] HcT[d, n] (HcT in the blocked B-operand layout, K = n_cp),
 // G read k-major from the same blocks.
-// k_parts: see launch_mfma_dh. `partial` is scratch of mfma_dw_partial_bytes() bytes (or NULL): with it, the tiles of a
+// `partial` is scratch of mfma_dw_partial_bytes() bytes (or NULL): with it, the tiles of a
 // sparsely filled last round are split along K over the idle compute units (cus = compute units
 // of the device).
 size_t mfma_dw_partial_bytes();
 void launch_mfma_dw(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D,
-                    const StoreSpec& out, float* partial, hipStream_t st, int k_parts = 0);
+                    const StoreSpec& out, float* partial, hipStream_t st);
 
 // Benchmark aid: device array of 12 counters (3 GEMM stages x {prologue, main loop, epilogue cycles, tiles})
 // that the whole-tile launches of the vocabulary, dH and dW GEMMs add to; NULL switches it off.

@@ -125,12 +125,12 @@ int dh_tail_parts(int cus, int tail, int k_slices, int64_t room) {
 
 template <int BL>
 void launch_dh(int cus, const void* G, int32_t Vp, const void* B, int64_t ldb, int b_rows, int32_t n_c, int32_t D,
-               const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st, int k_parts) {
+               const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st) {
     EpiStoreDH e{nullptr, reinterpret_cast<uint16_t*>(out.C), out.ldc, 0, out.row_map, row_scale, nullptr};
     const int tiles_m = (int)ceil_div(n_c, CfgGrad::BM), tiles_n = (int)ceil_div(D, CfgGrad::BN);
     const int tiles = tiles_m * tiles_n;
     const int tail = cus > 0 ? tiles % cus : 0;
-    const int parts = k_parts > 0 ? k_parts : partial ? dh_tail_parts(cus, tail, Vp / CfgGrad::BK, partial_floats / (CfgGrad::BM * CfgGrad::BN)) : 1;
+    const int parts = partial ? dh_tail_parts(cus, tail, Vp / CfgGrad::BK, partial_floats / (CfgGrad::BM * CfgGrad::BN)) : 1;
     if (parts == 1) {
         launch<CfgGrad, A_BLK_ROWS, WG_RANGES, BL>(G, Vp, B, ldb, n_c, D, Vp, e, st, 0, -1, 1, PHASE_DH, b_rows);
         return;
@@ -139,19 +139,17 @@ void launch_dh(int cus, const void* G, int32_t Vp, const void* B, int64_t ldb, i
     EpiStoreDH ep = e;
     ep.partial = partial;
     launch<CfgGrad, A_BLK_ROWS, WG_RANGES, BL>(G, Vp, B, ldb, n_c, D, Vp, ep, st, tiles - tail, tail, parts, -1, b_rows);
-    sum_partial_tiles_kernel<CfgGrad><<<dim3(tail, CfgGrad::BM / SUM_ROWS), 256, 0, st>>>(
+    sum_partial_tiles_kernel<CfgGrad><<<dim3(tail, CfgGrad::BM / sum_rows<CfgGrad>()), 256, 0, st>>>(
         partial, tiles - tail, parts, tiles_m, tiles_n, nullptr, out.ldc, n_c, D, 0, reinterpret_cast<uint16_t*>(out.C),
         out.row_map, row_scale);
 }
 }  // namespace
 
 void launch_mfma_dh(int cus, const void* G, int32_t Vp, const void* WT, const void* W, int32_t V, int32_t n_c, int32_t D,
-                    const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st, int k_parts) {
-    if (WT) launch_dh<B_BLK>(cus, G, Vp, WT, 0, 0, n_c, D, row_scale, out, partial, partial_floats, st, k_parts);
-    else launch_dh<B_KM>(cus, G, Vp, W, D, V, n_c, D, row_scale, out, partial, partial_floats, st, k_parts);
+                    const float* row_scale, const StoreSpec& out, float* partial, int64_t partial_floats, hipStream_t st) {
+    if (WT) launch_dh<B_BLK>(cus, G, Vp, WT, 0, 0, n_c, D, row_scale, out, partial, partial_floats, st);
+    else launch_dh<B_KM>(cus, G, Vp, W, D, V, n_c, D, row_scale, out, partial, partial_floats, st);
 }
-
-int mfma_dh_tiles(int32_t n_c, int32_t D) { return (int)(ceil_div(n_c, CfgGrad::BM) * ceil_div(D, CfgGrad::BN)); }
 
 // Whether dW's tiles are walked by resident workgroups, one per compute unit, that load a tile's first slices while the one
 // before is stored. Added to what is there, that hides the reading of the old values, until a long chunk's shared panels
@@ -167,9 +165,9 @@ static bool dw_resident(int32_t tokens, int accumulate) {
 }
 
 void launch_mfma_dw(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D,
-                    const StoreSpec& out, float* partial, hipStream_t st, int k_parts) {
+                    const StoreSpec& out, float* partial, hipStream_t st) {
     EpiStoreDW e{reinterpret_cast<float*>(out.C), nullptr, out.ldc, out.accumulate, nullptr, nullptr, nullptr};
-    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, dw_resident(n_cp, out.accumulate), st, k_parts);
+    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, dw_resident(n_cp, out.accumulate), st);
 }
 
 // Register-only loop of the GEMMs' MFMA instruction (8 wavefronts per compute unit, 32 independent

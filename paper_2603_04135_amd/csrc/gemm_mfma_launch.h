@@ -63,11 +63,11 @@ void launch(const void* A, int64_t lda, const void* B, int64_t ldb, int M, int N
 }
 
 // Sums the k_parts partial tiles of each of the n_tiles tiles from tile0 on, in part order, into
-// C (overwrite or accumulate). One workgroup per SUM_ROWS rows of a tile, a 16-byte vector per thread; N and ldc
+// C (overwrite or accumulate). One workgroup per sum_rows<Cfg>() rows of a tile, a 16-byte vector per thread; N and ldc
 // multiples of 4.
 // With Cb != NULL the sums go out as bf16 instead: row m times row_scale[m] (if not NULL) to row
 // row_map[m] (if not NULL) of Cb.
-constexpr int SUM_ROWS = 4;
+template <class Cfg> constexpr int sum_rows() { return 256 / (Cfg::BN / 4); }
 template <class Cfg>
 __global__ __launch_bounds__(256) void sum_partial_tiles_kernel(const float* __restrict__ partial, int tile0,
                                                                 int k_parts, int tiles_m, int tiles_n, float* C,
@@ -79,8 +79,8 @@ __global__ __launch_bounds__(256) void sum_partial_tiles_kernel(const float* __r
     int tm, tn;
     tile_coords<Cfg::GROUP_M>(tile0 + blockIdx.x, tiles_m, tiles_n, tm, tn);
     const float* src = partial + (size_t)blockIdx.x * k_parts * (Cfg::BM * Cfg::BN);
-    static_assert(SUM_ROWS * VPR == 256, "one vector per thread");
-    const int r = blockIdx.y * SUM_ROWS + threadIdx.x / VPR, cv = threadIdx.x % VPR;
+    static_assert(sum_rows<Cfg>() * VPR == 256 && Cfg::BM % sum_rows<Cfg>() == 0, "one vector per thread");
+    const int r = blockIdx.y * sum_rows<Cfg>() + threadIdx.x / VPR, cv = threadIdx.x % VPR;
     const int row = tm * Cfg::BM + r, col = tn * Cfg::BN + cv * 4;
     if (row >= M || col >= N) return;
     f32x4v v = *reinterpret_cast<const f32x4v*>(src + (size_t)r * Cfg::BN + cv * 4);
@@ -110,14 +110,14 @@ hipError_t allow_lds() {
 
 // dW[V, D] of a chunk by epilogue Epi (EpiStore<0>: float32, EpiStore<2>: bfloat16, overwritten): G is read k-major from its blocks.
 // The tiles of a sparsely filled last round are cut along K where `partial` is scratch for the partial tiles
-// (mfma_dw_partial_bytes), which a second kernel adds up; k_parts > 0: all tiles, fewer than compute units, into that many. resident: at
-// most one workgroup per compute unit, which walks the tiles.
+// (mfma_dw_partial_bytes), which a second kernel adds up. resident: at most one workgroup per compute unit, which walks the
+// tiles.
 template <class Epi>
 void launch_dw_tiles(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, const Epi& e, float* partial,
-                     bool resident, hipStream_t st, int k_parts = 0) {
+                     bool resident, hipStream_t st) {
     const int tiles_m = (int)ceil_div(V, CfgGrad::BM), tiles_n = (int)ceil_div(D, CfgGrad::BN);
     const int tiles = tiles_m * tiles_n, tail = cus > 0 ? tiles % cus : 0;
-    const int parts = k_parts > 0 ? k_parts : partial ? mfma_tail_parts(cus, tail, n_cp / CfgGrad::BK) : 1;
+    const int parts = partial ? mfma_tail_parts(cus, tail, n_cp / CfgGrad::BK) : 1;
     const int workgroups = resident ? cus : 0;
     const int whole = parts == 1 ? tiles : tiles - tail;
     launch<CfgGrad, A_BLK_KM, WG_RANGES, B_BLK>(G, Vp, HcT, 0, V, D, n_cp, e, st, 0, whole, 1, PHASE_DW, 0, workgroups);
@@ -125,7 +125,7 @@ void launch_dw_tiles(int cus, const void* G, int32_t Vp, const void* HcT, int32_
     Epi ep = e;
     ep.partial = partial;
     launch<CfgGrad, A_BLK_KM, WG_RANGES, B_BLK>(G, Vp, HcT, 0, V, D, n_cp, ep, st, whole, tail, parts);
-    sum_partial_tiles_kernel<CfgGrad><<<dim3(tail, CfgGrad::BM / SUM_ROWS), 256, 0, st>>>(
+    sum_partial_tiles_kernel<CfgGrad><<<dim3(tail, CfgGrad::BM / sum_rows<CfgGrad>()), 256, 0, st>>>(
         partial, whole, parts, tiles_m, tiles_n, e.Cf, e.ldc, V, D, e.accumulate, e.Cb, nullptr, nullptr);
 }
 

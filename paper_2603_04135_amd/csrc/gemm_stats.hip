@@ -17,6 +17,8 @@ typedef EpiStore<2> EpiStoreDW16;
 // 250, V = 40000 (157) 40 / 33.
 typedef PipeCfg<256, 64, 4, 2, 2, 4, 1> CfgGradFew;
 constexpr int GRAD_FEW_TILES = 128;
+typedef CfgFew<128> CfgSmall;
+static_assert(CfgSmall::BN == SMALL_BLOCK_ROWS && CfgSmall::BK == GEMM_B_BLOCK_K, "the blocks of HT");
 
 hipError_t allow_all() {
     hipError_t e = allow_logits<EpiStats<false, false>>();
@@ -24,6 +26,10 @@ hipError_t allow_all() {
     if (e == hipSuccess) e = allow_few<false, FewStats<false>>();
     if (e == hipSuccess) e = allow_lds<CfgBig, EpiStatsGrad>();
     if (e == hipSuccess) e = allow_lds<CfgGradFew, EpiStatsGrad>();
+    if (e == hipSuccess) e = allow_lds<CfgSmall, EpiStatsGradBoth, A_ROWS, WG_ROUNDS, B_MAP>();
+    if (e == hipSuccess) e = allow_lds<CfgSmall, EpiStoreDH, A_ROWS, WG_ROUNDS, B_KM>();
+    if (e == hipSuccess) e = allow_lds<CfgSmall, EpiStoreDW, A_ROWS, WG_RANGES, B_BLK>();
+    if (e == hipSuccess) e = allow_lds<CfgSmall, EpiStoreDW16, A_ROWS, WG_RANGES, B_BLK>();
     if (e == hipSuccess) e = allow_lds<CfgGrad, EpiStoreDW16, A_BLK_KM, WG_RANGES, B_BLK>();
     return e;
 }
@@ -69,9 +75,41 @@ void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc,
 }
 
 void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
-                         hipStream_t st, int k_parts) {
+                         hipStream_t st) {
     EpiStoreDW16 e{nullptr, reinterpret_cast<uint16_t*>(dW), D, 0, nullptr, nullptr, nullptr};
-    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, n_cp <= 2 * CfgGrad::BK, st, k_parts);
+    launch_dw_tiles(cus, G, Vp, HcT, n_cp, V, D, e, partial, n_cp <= 2 * CfgGrad::BK, st);
+}
+
+void launch_small_grad(const SmallGrad& s, const int32_t* y, const StatsGrad& g, hipStream_t st) {
+    EpiStatsGradBoth e{y, g, s.cv.n0, reinterpret_cast<uint16_t*>(s.G), s.Vk, reinterpret_cast<uint16_t*>(s.GT), s.n_sum};
+    launch<CfgSmall, A_ROWS, WG_ROUNDS, B_MAP>(s.W, s.D, s.H, s.D, s.V, s.cv.n_c, s.D, e, st, 0, -1, 1, -1, (int)s.h_rows, 0, s.map);
+}
+
+void launch_small_dh(const SmallGrad& s, const StoreSpec& out, int cus, hipStream_t st) {
+    const int tiles_m = (int)ceil_div(s.cv.n_c, CfgSmall::BM), tiles_n = (int)ceil_div(s.D, CfgSmall::BN), tiles = tiles_m * tiles_n;
+    const int parts = small_tiles_parts(cus, tiles, s.Vk / CfgSmall::BK);
+    EpiStoreDH e{nullptr, reinterpret_cast<uint16_t*>(out.C), out.ldc, 0, out.row_map, nullptr, parts > 1 ? s.partial : nullptr};
+    launch<CfgSmall, A_ROWS, WG_ROUNDS, B_KM>(s.G, s.Vk, s.W, s.D, s.cv.n_c, s.D, s.Vk, e, st, 0, tiles, parts, -1, s.V);
+    if (parts > 1)
+        sum_partial_tiles_kernel<CfgSmall><<<dim3(tiles, CfgSmall::BM / sum_rows<CfgSmall>()), 256, 0, st>>>(
+            s.partial, 0, parts, tiles_m, tiles_n, nullptr, out.ldc, s.cv.n_c, s.D, 0, e.Cb, out.row_map, nullptr);
+}
+
+void launch_small_dw(const SmallGrad& s, const StoreSpec& out, bool bf16, int cus, hipStream_t st) {
+    const int tiles_m = (int)ceil_div(s.V, CfgSmall::BM), tiles_n = (int)ceil_div(s.D, CfgSmall::BN), tiles = tiles_m * tiles_n;
+    const int parts = small_tiles_parts(cus, tiles, s.n_sum / CfgSmall::BK);
+    float *Cf = bf16 ? nullptr : reinterpret_cast<float*>(out.C), *partial = parts > 1 ? s.partial : nullptr;
+    uint16_t* Cb = bf16 ? reinterpret_cast<uint16_t*>(out.C) : nullptr;
+    if (bf16) {
+        EpiStoreDW16 e{Cf, Cb, out.ldc, 0, nullptr, nullptr, partial};
+        launch<CfgSmall, A_ROWS, WG_RANGES, B_BLK>(s.GT, s.n_sum, s.HT, 0, s.V, s.D, s.n_sum, e, st, 0, tiles, parts);
+    } else {
+        EpiStoreDW e{Cf, Cb, out.ldc, out.accumulate, nullptr, nullptr, partial};
+        launch<CfgSmall, A_ROWS, WG_RANGES, B_BLK>(s.GT, s.n_sum, s.HT, 0, s.V, s.D, s.n_sum, e, st, 0, tiles, parts);
+    }
+    if (parts > 1)
+        sum_partial_tiles_kernel<CfgSmall><<<dim3(tiles, CfgSmall::BM / sum_rows<CfgSmall>()), 256, 0, st>>>(
+            s.partial, 0, parts, tiles_m, tiles_n, Cf, out.ldc, s.V, s.D, out.accumulate, Cb, nullptr, nullptr);
 }
 
 }  // namespace dppo

@@ -18,8 +18,9 @@ struct Regions {                            // offsets into the workspace
     int32_t Vp, n_cp;
     size_t row_bytes;
     size_t o_hc, o_scale, o_z, o_pstats, o_pkeys, o_mx, o_sd, o_zy, o_tau;                    // forward
-    size_t o_wt, o_dwpart, o_dwacc, o_hct, o_fpart, o_y, o_rowc;                         // backward
+    size_t o_wt, o_dwpart, o_dwacc, o_hct, o_gt, o_fpart, o_y, o_rowc;                      // backward
     bool direct_w;
+    bool small;                             // the gradient by small tiles (see SmallGrad), of one chunk
     int f32_parts;
     size_t total;
 };
@@ -53,14 +54,16 @@ void layout(const dppo_head_shape& s, int32_t top_k, int what, int32_t n_cp, Reg
         r.total = off;
         return;
     }
-    r.direct_w = reads_w_directly(s.N, s.D);
     const bool bf16 = s.dtype == BF16;
+    r.small = bf16 && n_cp >= s.N && small_grad(s.N, s.D, s.V);
+    r.direct_w = r.small || reads_w_directly(s.N, s.D);
     r.o_wt = take(bf16 && !r.direct_w ? gemm_b_blocked_elems(s.D, r.Vp) * 2 : 0);
     r.o_dwpart = take(bf16 ? mfma_dw_partial_bytes() : 0);
     r.o_dwacc = take(what == BACKWARD_BF16_DW && n_cp < s.N ? (size_t)s.V * s.D * 4 : 0);
     r.o_hc = take(n * r.row_bytes);
     r.o_hct = take(bf16 ? gemm_b_blocked_elems(s.D, n_cp) * 2 : 0);
     r.o_z = take(n * r.Vp * element_bytes(s.dtype));
+    r.o_gt = take(r.small ? (size_t)round_up32(s.N, GEMM_B_BLOCK_K) * s.V * 2 : 0);
     const int64_t max_parts = r.Vp / s.D, k_parts = gemm_f32_max_parts(s.V);
     r.f32_parts = bf16 ? 0 : (int)(max_parts < k_parts ? max_parts : k_parts);
     r.o_fpart = take(r.f32_parts > 1 ? (size_t)r.f32_parts * n * s.D * 4 : 0);
@@ -210,7 +213,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
         if (gather && (map || logp)) {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
             float* scale = reinterpret_cast<float*>(w + r.o_scale);
-            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0, nullptr, 0};
+            GatherRows gr{tokens, r.row_bytes, h_scale, map ? w + r.o_hc : nullptr, y, nullptr, s.dtype == I8 ? scale : nullptr, nullptr, 0, nullptr, 0, 0};
             launch_stats_gather(gr, cv, st);
             if (map) { g.H = w + r.o_hc; g.h_rows = cv.n_c; g.map = nullptr; }
             if (map) { sc.h = scale; sc.map = nullptr; sc.rows = cv.n_c; }
@@ -291,8 +294,9 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
         const int32_t n_sum = round_up32(cv.n_c, GEMM_B_BLOCK_K);
         {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-            launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
-                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0, s.dtype == BF16 ? w + r.o_hct : nullptr, n_sum}, cv, st);
+            launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, r.small ? nullptr : Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
+                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0, s.dtype == BF16 ? w + r.o_hct : nullptr, n_sum,
+                                           r.small ? SMALL_BLOCK_ROWS : GEMM_B_BLOCK_ROWS}, cv, st);
         }
         StoreSpec oh{loss_pos ? dH : reinterpret_cast<char*>(dH) + (size_t)n0 * r.row_bytes, s.D, 0, loss_pos ? rowc : nullptr};
         StoreSpec ow{dw_sum, s.D, n0 == 0 && !p->accumulate_dW ? 0 : 1, nullptr};
@@ -312,6 +316,21 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
                             cus, st);
             continue;
         }
+        if (r.small) {
+            const SmallGrad sg{W, s.V, s.D, H, loss_pos ? s.T : (int64_t)cv.n_c, loss_pos, cv, n_sum, round_up32(s.V, GEMM_B_BLOCK_K),
+                               G, w + r.o_gt, w + r.o_hct, reinterpret_cast<float*>(w + r.o_dwpart)};
+            {
+                StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
+                launch_small_grad(sg, y, grad, st);
+            }
+            {
+                StageTimer tm(DPPO_STAGE_DH_GEMM, st);
+                launch_small_dh(sg, oh, cus, st);
+            }
+            StageTimer tm(DPPO_STAGE_DW_GEMM, st);
+            launch_small_dw(sg, ow, dw16, cus, st);
+            continue;
+        }
         {
             StageTimer tm(DPPO_STAGE_LOGITS_GEMM, st);
             launch_mfma_stats_grad(W, s.V, s.D, Hc, cv, y, grad, G, r.Vp, st);
@@ -324,15 +343,11 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
             int64_t floats = (int64_t)(mfma_dw_partial_bytes() / 4);
             const int64_t dw_floats = (int64_t)s.V * s.D / (dw16 && one_chunk ? 2 : 1);
             if (!ow.accumulate && dw_floats > floats) { dh_partial = dw_sum; floats = dw_floats; }
-            const int tiles = mfma_dh_tiles(cv.n_c, s.D);
-            launch_mfma_dh(cus, G, r.Vp, r.direct_w ? nullptr : w + r.o_wt, W, s.V, cv.n_c, s.D, nullptr, oh, dh_partial, floats, st,
-                           2 * tiles <= cus ? few_tiles_parts(cus, tiles, r.Vp / GEMM_B_BLOCK_K) : 0);
+            launch_mfma_dh(cus, G, r.Vp, r.direct_w ? nullptr : w + r.o_wt, W, s.V, cv.n_c, s.D, nullptr, oh, dh_partial, floats, st);
         }
         StageTimer tm(DPPO_STAGE_DW_GEMM, st);
-        const int dw_tiles = mfma_dh_tiles(s.V, s.D);
-        const int dw_parts = 2 * dw_tiles <= cus ? few_tiles_parts(cus, dw_tiles, n_sum / GEMM_B_BLOCK_K) : 0;
-        if (dw16 && one_chunk) launch_mfma_dw_bf16(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, dW, partial, st, dw_parts);
-        else launch_mfma_dw(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, ow, partial, st, dw_parts);
+        if (dw16 && one_chunk) launch_mfma_dw_bf16(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, dW, partial, st);
+        else launch_mfma_dw(cus, G, r.Vp, w + r.o_hct, n_sum, s.V, s.D, ow, partial, st);
     }
     if (dw16 && !one_chunk && s.N > 0) {
         StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);

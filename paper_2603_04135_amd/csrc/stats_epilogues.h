@@ -311,6 +311,55 @@ struct EpiStatsGrad {
     static constexpr bool SWAP = false;
 };
 
+// The same entries row-major, straight from the registers: G[n, v] (pitch ldg, zero from V on) and their transpose GT[v, n] (pitch ldt, zero
+// from the N-th token on, both), 8 bytes a lane each.
+struct EpiStatsGradBoth {
+    const int32_t* y; StatsGrad grad; int64_t n0;
+    uint16_t* G; int64_t ldg; uint16_t* GT; int64_t ldt;
+
+    __device__ __forceinline__ void look_up(int, int) const {}
+    template <class Cfg>
+    __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            const int n = c.n0 + ni * MB + acc_col(c.lane);
+            const bool token = n < c.N;
+            TokenGrad t{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+            int target = -1;
+            if (token) {
+                t = load_grad(grad, n0 + n);
+                target = y[n];
+            }
+#pragma unroll
+            for (int mi = 0; mi < Cfg::MI; ++mi) {
+                const int v = c.m0 + mi * MB + acc_row(c.lane, 0);
+                uint32_t w[2];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float lp = acc[mi][ni][q] - t.lse, g = grad_entry(t, lp, exp_fast(lp), v + q == target);
+                    const __bf16 b = (__bf16)(token && v + q < c.M ? g : 0.0f);
+                    const uint32_t h = __builtin_bit_cast(uint16_t, b);
+                    w[q / 2] = q % 2 ? w[q / 2] | h << 16 : h;
+                }
+                if (n < ldt && v < ldg) *reinterpret_cast<uint2*>(G + (size_t)n * ldg + v) = make_uint2(w[0], w[1]);
+                // the 4 x 4 entries of four neighbouring lanes transposed: lane i of them gets row v + i. First pairs of lanes: the even
+                // one rows 0 and 2, the odd one rows 1 and 3; then pairs of pairs.
+                const uint32_t o0 = xor_lane<1>(w[0]), o1 = xor_lane<1>(w[1]);
+                const bool odd = c.lane & 1, upper = c.lane & 2;
+                const uint32_t x = odd ? o0 >> 16 | (w[0] & 0xffff0000u) : (w[0] & 0xffffu) | o0 << 16;
+                const uint32_t z = odd ? o1 >> 16 | (w[1] & 0xffff0000u) : (w[1] & 0xffffu) | o1 << 16;
+                const uint32_t px = xor_lane<2>(x), pz = xor_lane<2>(z);
+                const int row = v + (c.lane & 3), col = c.n0 + ni * MB + (c.lane & 12);
+                if (row < c.M && col < ldt) *reinterpret_cast<uint2*>(GT + (size_t)row * ldt + col) = upper ? make_uint2(pz, z) : make_uint2(x, px);
+            }
+        }
+    }
+
+    template <class Cfg>
+    static constexpr int lds_bytes() { return 0; }
+    static constexpr bool SWAP = false;
+};
+
 }  // namespace mfma
 
 namespace {

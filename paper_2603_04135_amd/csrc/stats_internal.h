@@ -62,7 +62,7 @@ struct GatherRows {
     void* out; int32_t* y; int32_t* rowc; float* scale_out;
     void* clear; size_t clear_bytes;        // cleared by further workgroups of the launch
     // bfloat16: the rows' transpose [D, transpose_cols] in the blocked B-operand layout, zero from n_c on, by further workgroups too (NULL: none)
-    void* transpose; int32_t transpose_cols;
+    void* transpose; int32_t transpose_cols, transpose_block;      // transpose_block: rows of a block
 };
 void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st);
 
@@ -153,15 +153,32 @@ void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc,
                             int32_t Vp, hipStream_t st);
 // launch_mfma_dw with a bfloat16 result, overwritten.
 void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
-                         hipStream_t st, int k_parts = 0);
-// Parts along K of a GEMM whose few tiles fill at most half the chip: least estimated time. A slice takes 1.1 us, a partial tile (512 KB
-// written and read) 0.13, the launch that sums them 4. Up to 256 partial tiles, as many as mfma_dw_partial_bytes() holds, each of 4 slices
-// or more. dH of 6 tokens, D = 576, V = 1496 (3 tiles of 24 slices) whole 30 us, in 6 parts 13 and 4 for the sum.
-inline int few_tiles_parts(int cus, int tiles, int slices) {
+                         hipStream_t st);
+// The gradient by tiles of 128 x 128, for problems that large ones leave much of the chip idle in: the entries row-major both ways, G[n_c, Vk]
+// and GT[V, n_sum] (Vk, n_sum: V, n_c up to multiples of 64, zero there), H's rows through a map. HT: see GatherRows::transpose, by blocks of
+// 128. One chunk, no more than a chip of large tiles of entries, and of dW few (or next to no sum to each). Large tiles / these: D = 512,
+// V = 5000: 60 tokens 44 / 34 us, 1000 80 / 59; D = 2560, V = 3000: 60 68 / 55, 2500 193 / 151; D = 256, V = 20000: 300 68 / 54; D = 1024, V =
+// 12000 (188 large tiles of dW): 600 99 / 86, 750 104 / 107; V = 32000 (500): 60 77 / 74, 500 135 / 150.
+struct SmallGrad {
+    const void* W; int32_t V, D;
+    const void* H; int64_t h_rows; const int32_t* map; ChunkView cv; int32_t n_sum, Vk;
+    void* G; void* GT; const void* HT; float* partial;
+};
+constexpr int32_t SMALL_BLOCK_ROWS = 128;
+inline bool small_grad(int64_t N, int32_t D, int32_t V) {
+    return ceil_div(V, 256) * ceil_div(N, 256) <= 256 && (N <= 64 || ceil_div(V, 256) * ceil_div(D, 256) <= 192);
+}
+void launch_small_grad(const SmallGrad& s, const int32_t* y, const StatsGrad& g, hipStream_t st);
+void launch_small_dh(const SmallGrad& s, const StoreSpec& out, int cus, hipStream_t st);
+void launch_small_dw(const SmallGrad& s, const StoreSpec& out, bool bf16, int cus, hipStream_t st);
+// Parts along K of a GEMM of few tiles of 128 x 128: least estimated time of a slice's 0.45 us, 0.033 a partial tile (64 KB written and
+// read) and 4 for the launch that sums them. Two workgroups a compute unit, 4 slices or more each; 64 MB of partial tiles at most.
+inline int small_tiles_parts(int cus, int tiles, int slices) {
+    const int slots = 2 * (cus < 256 ? cus : 256);
     int best = 1;
-    double best_t = 1.1 * slices;
-    for (int p = 2; p <= slices / 4 && tiles * p <= (cus < 256 ? cus : 256); ++p) {
-        const double t = 1.1 * ((slices + p - 1) / p) + 4.0 + 0.13 * tiles * p;
+    double best_t = 0.45 * slices * (double)((tiles + slots - 1) / slots);
+    for (int p = 2; p <= slices / 4 && tiles * p <= slots; ++p) {
+        const double t = 0.45 * ((slices + p - 1) / p) + 4.0 + 0.033 * tiles * p;
         if (t < best_t) { best_t = t; best = p; }
     }
     return best;

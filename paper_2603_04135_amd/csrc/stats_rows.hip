@@ -342,8 +342,8 @@ __device__ void transpose_tokens(const GatherRows& g, ChunkView cv, int block, u
 #pragma unroll
         for (int k = 0; k < 4; ++k) w[k] = (uint32_t)tile[vec * 8 + 2 * k][cc] | ((uint32_t)tile[vec * 8 + 2 * k + 1][cc] << 16);
         static_assert(GEMM_B_BLOCK_K == 64, "a 64-column tile = one block column");
-        const size_t off = ((size_t)(drow / GEMM_B_BLOCK_ROWS) * (g.transpose_cols / GEMM_B_BLOCK_K) + r0 / GEMM_B_BLOCK_K) *
-                               (GEMM_B_BLOCK_ROWS * GEMM_B_BLOCK_K) + (size_t)(drow % GEMM_B_BLOCK_ROWS) * GEMM_B_BLOCK_K + vec * 8;
+        const size_t off = (((size_t)(drow / g.transpose_block) * (g.transpose_cols / GEMM_B_BLOCK_K) + r0 / GEMM_B_BLOCK_K) * g.transpose_block +
+                            drow % g.transpose_block) * GEMM_B_BLOCK_K + vec * 8;
         *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.transpose) + off) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }

@@ -735,3 +735,28 @@ def test_gradient_in_parts(P, N, D, V, out):
     check_grads(c, g, r)
     for room in (room_h, room_w):
         assert (room[:pad] == 7).all() and (room[-pad:] == 7).all()
+
+
+@pytest.mark.parametrize("N,D,V", [(3, 64, 70001), (64, 320, 3001), (65, 320, 3001), (100, 64, 60001), (70, 1024, 16001), (1500, 64, 20001),
+                                   (129, 128, 127), (1025, 448, 130)])
+@pytest.mark.parametrize("positions", [True, False])
+def test_gradient_of_every_tile(P, N, D, V, positions):
+    """Small and large tiles, one or several along every side, with and without positions; what is beside dH and dW stays."""
+    c = Case("bf16", N, D, V, seed=37, extra=None if positions else 0)
+    g = make_grads(c, 8, ALL)
+    pad = 512
+    first = None
+    for out in (torch.float32, torch.bfloat16):
+        room_h = torch.full((c.T * D + 2 * pad,), 7.0, dtype=torch.bfloat16, device=DEV)
+        room_w = torch.full((V * D + 2 * pad,), 7.0, dtype=out, device=DEV)
+        r = backward(P, c, g, dH=room_h[pad:-pad].view(c.T, D), dW=room_w[pad:-pad].view(V, D))
+        check_grads(c, g, r)
+        for room in (room_h, room_w):
+            assert (room[:pad] == 7).all() and (room[-pad:] == 7).all()
+        again = backward(P, c, g, dW_dtype=out)
+        assert torch.equal(r["dH"], again["dH"]) and torch.equal(r["dW"], again["dW"])
+        if first is not None:                    # (the same float32 sums, rounded once)
+            assert torch.equal(first["dH"], r["dH"]) and torch.equal(first["dW"].to(torch.bfloat16), r["dW"])
+        first = r
+    dW0 = torch.randn(c.W.shape, device=DEV)
+    check_grads(c, g, backward(P, c, g, dW=dW0.clone(), accumulate_dW=True), dW0)
