@@ -311,7 +311,58 @@ struct EpiStatsGrad {
     static constexpr bool SWAP = false;
 };
 
-// The same entries row-major, straight from the registers: G[n, v] (pitch ldg, zero from V on) and their transpose GT[v, n] (pitch ldt, zero
+// Four rows' bfloat16 values of a column (lane), rows 0, 1 and 2, 3 packed in w0 and w1, to four neighbouring columns of row (lane & 3): the
+// 4 x 4 values of four lanes transposed. First pairs of lanes: the even one rows 0 and 2, the odd one rows 1 and 3; then pairs of pairs.
+__device__ __forceinline__ uint2 transpose4(uint32_t w0, uint32_t w1, int lane) {
+    const uint32_t o0 = xor_lane<1>(w0), o1 = xor_lane<1>(w1);
+    const bool odd = lane & 1, upper = lane & 2;
+    const uint32_t x = odd ? o0 >> 16 | (w0 & 0xffff0000u) : (w0 & 0xffffu) | o0 << 16;
+    const uint32_t z = odd ? o1 >> 16 | (w1 & 0xffff0000u) : (w1 & 0xffffu) | o1 << 16;
+    const uint32_t px = xor_lane<2>(x), pz = xor_lane<2>(z);
+    return upper ? make_uint2(pz, z) : make_uint2(x, px);
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return (uint32_t)as_out(a, uint16_t()) | (uint32_t)as_out(b, uint16_t()) << 16; }
+
+// dH by small tiles: bfloat16 rows (all of a lane's entries of row_map at once, 8-byte stores), or, with `partial`, the raw tile as EpiStore's.
+struct EpiRows {
+    uint16_t* C; int64_t ldc; const int32_t* row_map; float* partial;
+
+    template <class Cfg>
+    __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        if (partial) {
+            float* dst = partial + (size_t)c.slot * (Cfg::BM * Cfg::BN) + c.wave_n * Cfg::WTN + acc_col(c.lane);
+#pragma unroll
+            for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int ni = 0; ni < Cfg::NI; ++ni)
+                        dst[(size_t)(c.wave_m * Cfg::WTM + mi * MB + acc_row(c.lane, j)) * Cfg::BN + ni * MB] = acc[mi][ni][j];
+            return;
+        }
+        int64_t to[Cfg::MI];
+#pragma unroll
+        for (int mi = 0; mi < Cfg::MI; ++mi) {
+            const int row = c.m0 + mi * MB + acc_row(c.lane, 0) + (c.lane & 3);
+            to[mi] = row < c.M ? (row_map ? (int64_t)row_map[row] : (int64_t)row) : -1;
+        }
+#pragma unroll
+        for (int mi = 0; mi < Cfg::MI; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < Cfg::NI; ++ni) {
+                const f32x4 v = acc[mi][ni];
+                const uint2 w = transpose4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), c.lane);
+                const int col = c.n0 + ni * MB + (c.lane & 12);
+                if (to[mi] >= 0 && col < c.N) *reinterpret_cast<uint2*>(C + (size_t)to[mi] * ldc + col) = w;
+            }
+    }
+
+    template <class Cfg>
+    static constexpr int lds_bytes() { return 0; }
+    static constexpr bool SWAP = false;
+};
+
+// EpiStatsGrad's entries row-major, straight from the registers: G[n, v] (pitch ldg, zero from V on) and their transpose GT[v, n] (pitch ldt, zero
 // from the N-th token on, both), 8 bytes a lane each.
 struct EpiStatsGradBoth {
     const int32_t* y; StatsGrad grad; int64_t n0;
@@ -320,37 +371,34 @@ struct EpiStatsGradBoth {
     __device__ __forceinline__ void look_up(int, int) const {}
     template <class Cfg>
     __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
+        TokenGrad tokens[Cfg::NI];               // (of all columns at once; beyond the last token its own)
+        int targets[Cfg::NI];
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            const int n = c.n0 + ni * MB + acc_col(c.lane), in = n < c.N ? n : c.N - 1;
+            tokens[ni] = load_grad(grad, n0 + in);
+            targets[ni] = y[in];
+        }
 #pragma unroll
         for (int ni = 0; ni < Cfg::NI; ++ni) {
             const int n = c.n0 + ni * MB + acc_col(c.lane);
             const bool token = n < c.N;
-            TokenGrad t{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-            int target = -1;
-            if (token) {
-                t = load_grad(grad, n0 + n);
-                target = y[n];
-            }
+            const TokenGrad t = tokens[ni];
 #pragma unroll
             for (int mi = 0; mi < Cfg::MI; ++mi) {
                 const int v = c.m0 + mi * MB + acc_row(c.lane, 0);
                 uint32_t w[2];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float lp = acc[mi][ni][q] - t.lse, g = grad_entry(t, lp, exp_fast(lp), v + q == target);
+                    const float lp = acc[mi][ni][q] - t.lse, g = grad_entry(t, lp, exp_fast(lp), v + q == targets[ni]);
                     const __bf16 b = (__bf16)(token && v + q < c.M ? g : 0.0f);
                     const uint32_t h = __builtin_bit_cast(uint16_t, b);
                     w[q / 2] = q % 2 ? w[q / 2] | h << 16 : h;
                 }
                 if (n < ldt && v < ldg) *reinterpret_cast<uint2*>(G + (size_t)n * ldg + v) = make_uint2(w[0], w[1]);
-                // the 4 x 4 entries of four neighbouring lanes transposed: lane i of them gets row v + i. First pairs of lanes: the even
-                // one rows 0 and 2, the odd one rows 1 and 3; then pairs of pairs.
-                const uint32_t o0 = xor_lane<1>(w[0]), o1 = xor_lane<1>(w[1]);
-                const bool odd = c.lane & 1, upper = c.lane & 2;
-                const uint32_t x = odd ? o0 >> 16 | (w[0] & 0xffff0000u) : (w[0] & 0xffffu) | o0 << 16;
-                const uint32_t z = odd ? o1 >> 16 | (w[1] & 0xffff0000u) : (w[1] & 0xffffu) | o1 << 16;
-                const uint32_t px = xor_lane<2>(x), pz = xor_lane<2>(z);
+                const uint2 t4 = transpose4(w[0], w[1], c.lane);
                 const int row = v + (c.lane & 3), col = c.n0 + ni * MB + (c.lane & 12);
-                if (row < c.M && col < ldt) *reinterpret_cast<uint2*>(GT + (size_t)row * ldt + col) = upper ? make_uint2(pz, z) : make_uint2(x, px);
+                if (row < c.M && col < ldt) *reinterpret_cast<uint2*>(GT + (size_t)row * ldt + col) = t4;
             }
         }
     }

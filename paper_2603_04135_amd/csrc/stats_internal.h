@@ -157,8 +157,8 @@ void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, in
 // The gradient by tiles of 128 x 128, for problems that large ones leave much of the chip idle in: the entries row-major both ways, G[n_c, Vk]
 // and GT[V, n_sum] (Vk, n_sum: V, n_c up to multiples of 64, zero there), H's rows through a map. HT: see GatherRows::transpose, by blocks of
 // 128. One chunk, no more than a chip of large tiles of entries, and of dW few (or next to no sum to each). Large tiles / these: D = 512,
-// V = 5000: 60 tokens 44 / 34 us, 1000 80 / 59; D = 2560, V = 3000: 60 68 / 55, 2500 193 / 151; D = 256, V = 20000: 300 68 / 54; D = 1024, V =
-// 12000 (188 large tiles of dW): 600 99 / 86, 750 104 / 107; V = 32000 (500): 60 77 / 74, 500 135 / 150.
+// V = 5000: 60 tokens 44 / 30 us, 1000 80 / 58; D = 2560, V = 3000: 60 68 / 52, 2500 193 / 149; D = 256, V = 20000: 300 68 / 52; D = 1024, V =
+// 12000 (188 large tiles of dW): 600 99 / 84, 750 104 / 107; V = 32000 (500): 60 77 / 74, 500 135 / 150.
 struct SmallGrad {
     const void* W; int32_t V, D;
     const void* H; int64_t h_rows; const int32_t* map; ChunkView cv; int32_t n_sum, Vk;
