@@ -257,18 +257,22 @@ struct EpiStatsGrad {
     template <class Cfg>
     __device__ __forceinline__ void run(f32x4 (&acc)[Cfg::MI][Cfg::NI], const TileCtx& c) const {
         constexpr int ZPITCH = StagedStore<Cfg>::ZPITCH;
+        // all columns' loads at once (beyond the last token its own)
+        TokenGrad tokens[Cfg::NI];
+        int targets[Cfg::NI];                                       // among the wavefront's rows
+#pragma unroll
+        for (int ni = 0; ni < Cfg::NI; ++ni) {
+            const int n = c.n0 + ni * MB + acc_col(c.lane), in = n < n_c ? n : n_c - 1;
+            tokens[ni] = load_grad(grad, n0 + in);
+            targets[ni] = n < n_c ? y[in] - c.m0 : -1;
+        }
         auto body = [&](auto full_tag) __attribute__((always_inline)) {
-            constexpr bool FULL = decltype(full_tag)::value;
+            constexpr bool FULL = decltype(full_tag)::value;        // neither vocabulary nor tokens end in the tile
 #pragma unroll
             for (int ni = 0; ni < Cfg::NI; ++ni) {
-                const int tok = c.wave_n * Cfg::WTN + ni * MB + acc_col(c.lane);
-                const int n = c.bn0 + tok;
-                TokenGrad t{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                int at = -1;                                        // target among the wavefront's rows
-                if (n < n_c) {
-                    t = load_grad(grad, n0 + n);
-                    at = y[n] - (c.bm0 + c.wave_m * Cfg::WTM);
-                }
+                const int tok = c.wave_n * Cfg::WTN + ni * MB + acc_col(c.lane), at = targets[ni];
+                const bool token = FULL || c.bn0 + tok < n_c;
+                const TokenGrad t = tokens[ni];
 #pragma unroll
                 for (int mi = 0; mi < Cfg::MI; ++mi) {
                     const int vloc = c.wave_m * Cfg::WTM + mi * MB + acc_row(c.lane, 0);
@@ -278,7 +282,7 @@ struct EpiStatsGrad {
                         const float lp = acc[mi][ni][q] - t.lse;
                         float g = grad_entry(t, lp, exp_fast(lp), false);
                         // (a padding token's row of zeros times a weight of -infinity is NaN, which dW would sum)
-                        g = n < n_c && (FULL || c.bm0 + vloc + q < V) ? g : 0.0f;
+                        g = token && (FULL || c.bm0 + vloc + q < V) ? g : 0.0f;
                         const __bf16 b = (__bf16)g;   // scalar copy: reading h[q] back right after writing it miscompiles
                         h[q] = b;
                     }
@@ -296,7 +300,7 @@ struct EpiStatsGrad {
                     }
             }
         };
-        if (c.bm0 + Cfg::BM <= V) body(std::true_type{});
+        if (c.bm0 + Cfg::BM <= V && c.bn0 + Cfg::BN <= n_c) body(std::true_type{});
         else body(std::false_type{});
         __syncthreads();
         const StagedStore<Cfg> staged(c, G, ldg);
