@@ -17,7 +17,7 @@
  *     word (dppo_pack: meta[3]; the LM-head calls: `status`) and leave the outputs defined;
  *   - the library keeps no state between calls except: the message of the last error
  *     (per thread), per-device kernel attributes and compute-unit count (looked up on the
- *     first bfloat16 LM-head call on each device), and the optional stage timing below;
+ *     first bfloat16 or int8 LM-head call on each device), and the optional stage timing below;
  *   - no C++ exception crosses this boundary.
  */
 #ifndef DPPO_H_
@@ -295,8 +295,8 @@ int dppo_loss_fwd_bwd(const dppo_head_shape* shape, const dppo_loss_params* p, i
  *   top_ids[n*top_k + i], top_logp[...] = id and log-probability of the i-th largest logit, equal logits in the
  *   order of their ids; 0 <= top_k <= min(DPPO_TOP_K_MAX, V), both NULL for 0.
  * Sums are float32 (against the maximum, so that neither lse nor entropy loses digits to large logits); logits at
- * -infinity carry no weight. A row with a NaN logit or one at +infinity has NaN results; its top_ids are still distinct
- * and in [0, V). V is at most 2^30. ws must be 256-byte aligned; a smaller workspace than recommended means
+ * -infinity carry no weight (a row of nothing else: lse -infinity, entropy and logp NaN). A row with a NaN logit or one at
+ * +infinity has NaN results. top_ids are distinct and in [0, V) for every row. V is at most 2^30. ws must be 256-byte aligned; a smaller workspace than recommended means
  * smaller token chunks and does not change what a token's results are, except for their last bits.
  */
 #define DPPO_TOP_K_MAX 64
@@ -319,7 +319,9 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k,
  *   dH[T,D] = dz W (dtype of H; rows that are no loss rows are zero),  dW[V,D] = dz^T H.
  * dW_dtype 0: float32, added to the buffer's contents if accumulate_dW != 0. dW_dtype 1: bfloat16 (bfloat16 operands only),
  * overwritten: the float32 sum over all tokens, rounded once. dW is used for partial sums of dH before it is written.
- * bfloat16 operands: dz is rounded to bfloat16 as an operand of the two products. dtype 2 has no gradient. */
+ * bfloat16 operands: dz is rounded to bfloat16 as an operand of the two products. dtype 2 has no gradient. A token whose lse or
+ * entropy is not finite (see above) has a NaN dz, which reaches all of dW: leave it out of loss_pos. Entries of loss_pos must be
+ * distinct here (not checked); dppo_token_stats takes them in any order and more than once. */
 typedef struct {
     int32_t accumulate_dW;
     int32_t dW_dtype;      /* 0 = float32, 1 = bfloat16 */
@@ -366,8 +368,8 @@ int dppo_token_norm_coef(int32_t Q, int32_t G, const int32_t* comp_len, const fl
                          void* stream);
 
 /* --------------------------------------------------------------------------------
- * Optional stage timing, for benchmarks. While enabled, dppo_token_logprob and
- * dppo_loss_fwd_bwd record a pair of HIP events around each launch of the stages below, on
+ * Optional stage timing, for benchmarks. While enabled, dppo_token_logprob, dppo_loss_fwd_bwd,
+ * dppo_token_stats, dppo_token_stats_bwd and dppo_matmul_i8 record a pair of HIP events around each launch of the stages below, on
  * the caller's stream (the kernels themselves are unchanged). dppo_timing_read waits for the
  * recorded events (a host-side wait), returns the summed milliseconds and the launch count
  * of every stage since the last reset, and with reset != 0 forgets them. Host arrays.
@@ -379,7 +381,7 @@ enum {
     DPPO_STAGE_GRAD_LOGITS = 1, /* softmax-gradient pass over the stored chunk (float32), row scales (bfloat16) */
     DPPO_STAGE_DH_GEMM = 2,     /* dH = G W                                               */
     DPPO_STAGE_DW_GEMM = 3,     /* dW += G^T H                                            */
-    DPPO_STAGE_ELEMENTWISE = 4, /* every other kernel of the two LM-head calls: row gather, transposes,
+    DPPO_STAGE_ELEMENTWISE = 4, /* every other kernel of the LM-head calls: row gather, transposes,
                                    target logits, combination of the per-tile statistics, token loss
                                    terms, zero fill of dH, the segmented reduction (HBM-bound)  */
     DPPO_N_STAGES = 5
