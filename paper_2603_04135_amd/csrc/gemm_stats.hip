@@ -19,7 +19,7 @@ typedef PipeCfg<256, 64, 4, 2, 2, 4, 1> CfgGradFew;
 constexpr int GRAD_FEW_TILES = 128;
 // Eight wavefronts: where there are few workgroups, the reads of four from LDS show (D = 512, V = 5000: entries of 60 tokens 12.7 / 9.4 us with
 // four / eight). Deeper rings of slices are no faster: two workgroups no longer fit a compute unit.
-typedef PipeCfg<128, 128, 2, 4, 2, 1, 1> CfgSmall;
+typedef Cfg128Eight CfgSmall;
 static_assert(CfgSmall::BN == SMALL_BLOCK_ROWS && CfgSmall::BK == GEMM_B_BLOCK_K, "the blocks of HT");
 
 hipError_t allow_all() {

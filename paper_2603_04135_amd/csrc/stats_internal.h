@@ -108,7 +108,8 @@ inline int32_t group_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : 
 // Groups of all tiles (the last may lie behind the vocabulary).
 inline int32_t groups_of_tiles(int tile, int32_t V) { return (int32_t)ceil_div(V, tile_rows(tile)) * (tile == TILE_FEW ? 1 : STATS_GROUPS); }
 // For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
-// kernel for few tokens hold. Up to 128 tokens as for the log-probabilities alone (see CfgFew). Beyond, the tile whose rounds of the chip
+// kernel for few tokens hold. Up to 128 tokens as for the log-probabilities alone (see CfgFew; by 128 columns where every tile has a compute
+// unit to itself). Beyond, the tile whose rounds of the chip
 // take the least time, 256 x 256 : 256 x 192 : two of 128 x 128 as 20 : 18 : 15, the last while large tiles fill no more than two rounds.
 // Statistics, 256 x 256 / 256 x 192 / 128 x 128, with the rounds of each: D = 1024, V = 32000: 224 tokens (1/1/1) 30 / 29 / 22 us, 384
 // (1/1/2) 34 / 29 / 34, 512 (1/2/2) 35 / 44 / 37, 576 (2/2/3) 54 / 44 / 48, 768 (2/2/3) 55 / 48 / 52, 1024 (2/3/4) 61 / 72 / 72, 1152
@@ -117,9 +118,9 @@ inline int32_t groups_of_tiles(int tile, int32_t V) { return (int32_t)ceil_div(V
 constexpr int64_t SMALL_TILES_MOST = 512;
 inline int logits_tile(int32_t n, int32_t V, int32_t k2, bool i8) {
     if (n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16)) return TILE_FEW;
-    if (n <= 96) return TILE_128x96;
-    if (n <= 128) return TILE_128x128;
     constexpr int64_t CHIP = 256;                 // compute units
+    if (n <= 96 && ceil_div(V, 128) > CHIP) return TILE_128x96;
+    if (n <= 128) return TILE_128x128;
     const int64_t rows = ceil_div(V, 256), large = rows * ceil_div(n, 256);
     const int64_t t256 = 20 * ceil_div(large, CHIP), t192 = 18 * ceil_div(rows * ceil_div(n, 192), CHIP);
     const int64_t t128 = 15 * ceil_div(ceil_div(V, 128) * ceil_div(n, 128), 2 * CHIP);
