@@ -92,14 +92,15 @@ __global__ __launch_bounds__(ROWS_THREADS) void stats_rows_kernel(const float* _
             for (int u = 0; u < ROWS_UNROLL; ++u) {
                 if (!__any(!(m4[u] < top.floor))) continue;
                 const int i = i0 + u * ROWS_THREADS + lane;
-                top.offer4(x[u], i * 4, i < hi ? a.V : 0, o.top_k, lane);
+                top.add4(x[u], i * 4, i < hi ? a.V : 0);
+                top.take(o.top_k, lane, 63);
             }
         }
     }
     s = join_lanes<1>(s);
     if (lane == 0) red[wave] = s;
     if (TOP) {
-        top.flush(o.top_k, lane);
+        top.take(o.top_k, lane, 0);
         lists[wave][lane] = top.entry;
     }
     __syncthreads();
@@ -143,8 +144,10 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
     TopList top(pending);
     if (TOP) {
         const int entries = partial.parts * o.top_k;
-        for (int i = 0; i < entries; i += 64) top.offer(i + lane < entries ? partial.keys[at * o.top_k + i + lane] : 0, o.top_k, lane);
-        top.flush(o.top_k, lane);
+        for (int i = 0; i < entries; i += 64) {
+            top.add(i + lane < entries ? partial.keys[at * o.top_k + i + lane] : 0);
+            top.take(o.top_k, lane, i + 64 < entries ? 63 : 0);
+        }
     }
     const int64_t gi = cv.n0 + n;
     float zy = 0.0f;
@@ -162,119 +165,110 @@ __global__ __launch_bounds__(64) void join_parts_kernel(const float* __restrict_
 // Joins the statistics of TOK tokens per workgroup over the groups of rows, and picks their top alternatives. The k largest logits of a
 // token lie in the k groups with the largest maxima (in the order of maximum, then group: every group ahead of another one holds a
 // logit that is ahead of all of the other's), so that of the stored logits only those groups are read: k / 2 KB of a row of V.
-// The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then 16 / TOK wavefronts per token
-// list the groups, and after that their logits. (Bound by latency up to some 2000 tokens.)
+// The workgroup reads the statistics, neighbouring tokens side by side, the maxima stay in LDS; then up to 16 / TOK wavefronts per token
+// list the groups, and after that their logits. Bound by latency up to some 2000 tokens, that of fetching its own code among it: both passes run
+// the same instructions (V = 3000, 1 and 20 alternatives, 256 tokens: 10.9 -> 8.2 and 11.4 -> 10.1 us against a pass of its own each).
 constexpr int JOIN_THREADS = 1024, JOIN_WAVES = JOIN_THREADS / 64, JOIN_MAXIMA = 10240, JOIN_UNROLL = 6;
 template <int TOK, bool TOP>
 __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part, int32_t rows, const float* __restrict__ Z, int64_t ldz,
                                                                   TokenArgs a, int look_up, StatsOut o, ChunkView cv) {
     constexpr int LANES = JOIN_THREADS / TOK, WPT = JOIN_WAVES / TOK;       // lanes and wavefronts per token
     constexpr int ROW = TOK + 1, BLOCK = JOIN_MAXIMA / TOK;                 // maxima in LDS: row pitch, groups of a block
-    __shared__ __attribute__((aligned(8))) float maxima[TOP ? BLOCK * ROW : 1];      // and then the logits that wait for a list
-    static_assert(BLOCK * ROW * 4 >= JOIN_WAVES * PENDING4 * 8, "LDS");
+    __shared__ float maxima[TOP ? BLOCK * ROW : 1];
     __shared__ Stats red[JOIN_WAVES][TOK];
     __shared__ Stats fin[TOK];
-    __shared__ uint64_t lists[TOP ? JOIN_WAVES : 1][PENDING];               // of the wavefronts: groups that wait, then lists that are shared
+    __shared__ uint64_t pending[TOP ? JOIN_WAVES : 1][PENDING4];
+    __shared__ uint64_t lists[TOP ? JOIN_WAVES : 1][TOP_MAX];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int tok = tid % TOK, n = blockIdx.x * TOK + tok;
     const int my_tok = wave / WPT, sub = wave % WPT, my_n = blockIdx.x * TOK + my_tok;   // of the wavefront's list
     const int groups = (a.V + rows - 1) / rows;
     Stats s = no_stats();
-    TopList top(lists[TOP ? wave : 0]);
-    for (int b0 = 0; b0 < groups; b0 += BLOCK) {
-        const int b1 = groups - b0 < BLOCK ? groups : b0 + BLOCK;
-        if (TOP && b0 > 0) __syncthreads();
-        if (n < cv.n_c) {
-            for (int g0 = b0 + tid / TOK; g0 < b1; g0 += LANES * JOIN_UNROLL) {
-                float2 sd[JOIN_UNROLL];
-                float m[JOIN_UNROLL];
+    auto load_block = [&](int b0, int b1) __attribute__((always_inline)) {
+        if (n >= cv.n_c) return;
+        for (int g0 = b0 + tid / TOK; g0 < b1; g0 += LANES * JOIN_UNROLL) {
+            float2 sd[JOIN_UNROLL];
+            float m[JOIN_UNROLL];
 #pragma unroll
-                for (int u = 0; u < JOIN_UNROLL; ++u) {
-                    const int g = g0 + u * LANES;
-                    if (g >= b1) break;
-                    m[u] = part.mx[part.at(g, n)];
-                    sd[u] = part.sd[part.at(g, n)];
-                }
+            for (int u = 0; u < JOIN_UNROLL; ++u) {
+                const int g = g0 + u * LANES;
+                if (g >= b1) break;
+                m[u] = part.mx[part.at(g, n)];
+                sd[u] = part.sd[part.at(g, n)];
+            }
 #pragma unroll
-                for (int u = 0; u < JOIN_UNROLL; ++u) {
-                    const int g = g0 + u * LANES;
-                    if (g >= b1) break;
-                    s = join(s, Stats{m[u], sd[u].x, sd[u].y});
-                    if (TOP) maxima[(g - b0) * ROW + tok] = m[u];
-                }
+            for (int u = 0; u < JOIN_UNROLL; ++u) {
+                const int g = g0 + u * LANES;
+                if (g >= b1) break;
+                s = join(s, Stats{m[u], sd[u].x, sd[u].y});
+                if (TOP) maxima[(g - b0) * ROW + tok] = m[u];
             }
         }
-        if (!TOP) continue;
+    };
+    auto finish_statistics = [&]() __attribute__((always_inline)) {
+        s = join_lanes<TOK>(s);
+        if (lane < TOK) red[wave][lane] = s;
         __syncthreads();
-        if (my_n < cv.n_c) {
-            if (b0 == 0 && b1 > 128) {
-                // the lanes' own maxima bound what is listed: a quarter more than k instead of k (1 + log(groups / k))
-                float m = -__builtin_inff();
-                for (int g = sub * 64 + lane; g < b1; g += WPT * 64) m = fmaxf(m, maxima[g * ROW + my_tok]);
-                top.at_least(kth_of_lanes(m, o.top_k, lane));
-            }
-            for (int g0 = b0 + sub * 64; g0 < b1; g0 += WPT * 64) {
-                const int g = g0 + lane;
-                top.offer(g < b1 ? top_key(maxima[(g - b0) * ROW + my_tok], (uint32_t)g) : 0, o.top_k, lane);
-            }
-            if (b1 == groups) top.flush(o.top_k, lane);
-        }
-    }
-    s = join_lanes<TOK>(s);
-    if (lane < TOK) red[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0) {
+        if (wave != 0) return;
         s = no_stats();
         for (int w = lane / TOK; w < JOIN_WAVES; w += 64 / TOK) s = join(s, red[w][tok]);
         s = join_lanes<TOK>(s);
-        if (lane < TOK) {
-            if (TOP) fin[tok] = s;
-            if (n < cv.n_c) {
-                const int64_t gi = cv.n0 + n;
-                if (look_up && a.status != nullptr) report_token(a, gi);
-                write_token(o, gi, s, part.zy ? part.zy[n] : 0.0f);
-            }
-        }
-    }
-    if (!TOP) return;
-    // the token's first wavefront ends with all of its lists joined
-    auto join_lists = [&](TopList& list) __attribute__((always_inline)) {
-#pragma unroll
-        for (int d = 1; d < WPT; d *= 2) {
-            if (d > 1) __syncthreads();
-            if (sub % (2 * d) == d) lists[wave][lane] = list.entry;
-            __syncthreads();
-            if (sub % (2 * d) == 0) list.merge(lists[wave + d][lane], lane);
+        if (lane >= TOK) return;
+        if (TOP) fin[tok] = s;
+        if (n < cv.n_c) {
+            const int64_t gi = cv.n0 + n;
+            if (look_up && a.status != nullptr) report_token(a, gi);
+            write_token(o, gi, s, part.zy ? part.zy[n] : 0.0f);
         }
     };
-    join_lists(top);
-    if (sub == 0) lists[wave][lane] = top.entry;
-    __syncthreads();
-    const uint64_t group = lists[wave - sub][lane];
-    // all of them read the groups' logits: all loads of 8 rounds under way at once, one round a lane's float4, rows / 4 lanes a group. (One
-    // round at a time is looked at by code that is there once: unrolled, it does not fit the instruction cache.)
-    constexpr int ROUNDS = 8;
-    TopList best(reinterpret_cast<uint64_t*>(maxima) + wave * PENDING4);
-    if (my_n < cv.n_c) {
-        const int count = groups < o.top_k ? groups : o.top_k;
-        // the k-th largest maximum: k logits are no smaller
-        if (count == o.top_k) best.at_least(lane_value(group, count - 1));
-        const float* z = Z + (size_t)my_n * ldz;
-        const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);
-        for (int i0 = sub * per; i0 < count; i0 += per * WPT * ROUNDS) {
-            float x[ROUNDS][4];
-            int v0[ROUNDS];
-#pragma unroll
-            for (int u = 0; u < ROUNDS; ++u) {
-                const int i = i0 + u * per * WPT + which;
-                const uint32_t g = top_index((uint64_t)(uint32_t)__shfl((int)(uint32_t)group, i < count ? i : 0, 64));
-                v0[u] = i < count ? (int)g * rows + in * 4 : a.V;
-                if (v0[u] < a.V) *reinterpret_cast<float4*>(x[u]) = *reinterpret_cast<const float4*>(z + v0[u]);
-            }
+    if (!TOP) {
+        load_block(0, groups);
+        finish_statistics();
+        return;
+    }
+    // Two passes of the same code: the token's `used` wavefronts list its groups, block by block, then the logits of those that are ahead.
+    TopList top(pending[TOP ? wave : 0]);
+    const int per = 256 / rows, in = lane % (rows / 4), which = lane / (rows / 4);      // groups of a round of logits, rows / 4 lanes a group
+    const float* z = Z + (size_t)my_n * ldz;
+    constexpr int ROUNDS = 6;                    // rounds of logits whose loads are under way at once, one round a lane's float4
+    float x[ROUNDS][4];
+    int v0[ROUNDS];
+    uint64_t group = 0;
+    bool logits = false;
+    int b0 = 0, b1 = 0, first = 0, end = 0, step = 0, used = 1;
+    while (used < WPT && used * 128 < groups) used *= 2;
+    while (true) {
+        bool more = false;                       // a further block of groups
+        if (!logits) {
+            if (b0 > 0) __syncthreads();
+            b1 = groups - b0 < BLOCK ? groups : b0 + BLOCK;
+            load_block(b0, b1);
+            __syncthreads();
+            first = b0 + sub * 64; end = b1; step = used * 64;
+            more = b1 < groups;
+        }
+        if (my_n >= cv.n_c || sub >= used) end = first;
+        int ring = 0;
 #pragma unroll 1
-            for (int i = i0; i < count && i < i0 + per * WPT * ROUNDS; i += per * WPT) {
+        for (int i = first;;) {
+            const bool valid = i < end;
+            if (valid && !logits) {
+                const int g = i + lane;
+                top.add(g < end ? top_key(maxima[(g - b0) * ROW + my_tok], (uint32_t)g) : 0);
+            }
+            if (valid && logits) {
+                if (ring == 0) {
+#pragma unroll
+                    for (int u = 0; u < ROUNDS; ++u) {
+                        const int at = i + u * step + which;
+                        const uint32_t g = top_index((uint64_t)(uint32_t)__shfl((int)(uint32_t)group, at < end ? at : 0, 64));
+                        v0[u] = at < end ? (int)g * rows + in * 4 : a.V;
+                        if (v0[u] < a.V) *reinterpret_cast<float4*>(x[u]) = *reinterpret_cast<const float4*>(z + v0[u]);
+                    }
+                }
+                ring = ring + 1 == ROUNDS ? 0 : ring + 1;
                 const float m = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3]));
-                if (__any(v0[0] < a.V && !(m < best.floor))) best.offer4(x[0], v0[0], a.V, o.top_k, lane);
+                if (__any(v0[0] < a.V && !(m < top.floor))) top.add4(x[0], v0[0], a.V);
 #pragma unroll
                 for (int u = 0; u + 1 < ROUNDS; ++u) {
                     v0[u] = v0[u + 1];
@@ -282,11 +276,38 @@ __global__ __launch_bounds__(JOIN_THREADS) void stats_join_kernel(StatsPart part
                     for (int q = 0; q < 4; ++q) x[u][q] = x[u + 1][q];
                 }
             }
+            i += step;
+            top.take(o.top_k, lane, i < end || more ? 63 : 0);
+            if (i >= end) break;
         }
-        best.flush(o.top_k, lane);
+        if (more) {
+            b0 += BLOCK;
+            continue;
+        }
+        // the token's first wavefront ends with all of its lists joined
+#pragma unroll 1
+        for (int d = 1; d < used; d *= 2) {
+            __syncthreads();
+            if ((sub & (2 * d - 1)) == d) lists[wave][lane] = top.entry;
+            __syncthreads();
+            if ((sub & (2 * d - 1)) == 0) top.merge(lists[wave + d][lane], lane);
+        }
+        if (logits) break;
+        if (sub == 0) lists[wave][lane] = top.entry;
+        finish_statistics();                     // (with a barrier in it)
+        group = lists[wave - sub][lane];
+        top = TopList(pending[TOP ? wave : 0]);
+        logits = true;
+        first = sub * per;
+        end = groups < o.top_k ? groups : o.top_k;
+        // the k-th largest maximum: k logits are no smaller
+        if (end == o.top_k) top.at_least(lane_value(group, end - 1));
+        used = 1;
+        while (used < WPT && used * per * 2 < end) used *= 2;
+        step = used * per;
     }
-    join_lists(best);
-    if (sub == 0 && my_n < cv.n_c) write_top(o, cv.n0 + my_n, fin[my_tok], best, lane);
+    __syncthreads();
+    if (sub == 0 && my_n < cv.n_c) write_top(o, cv.n0 + my_n, fin[my_tok], top, lane);
 }
 
 // tau[n]: one wavefront per token lists the maxima of the leading groups, read with neighbouring tokens side by side.
@@ -304,10 +325,11 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
             for (int g = g0 + tid / BOUND_TOK; g < g1; g += 1024 / BOUND_TOK) maxima[(g - g0) * (BOUND_TOK + 1) + tok] = part.mx[part.at(g, n)];
         }
         __syncthreads();
-        for (int i = g0; i < g1; i += 64)
-            top.offer(i + lane < g1 && my_n < n_c ? top_key(maxima[(i + lane - g0) * (BOUND_TOK + 1) + wave], (uint32_t)(i + lane)) : 0, top_k, lane);
+        for (int i = g0; i < g1; i += 64) {
+            top.add(i + lane < g1 && my_n < n_c ? top_key(maxima[(i + lane - g0) * (BOUND_TOK + 1) + wave], (uint32_t)(i + lane)) : 0);
+            top.take(top_k, lane, i + 64 < groups ? 63 : 0);
+        }
     }
-    top.flush(top_k, lane);
     if (lane == 0 && my_n < n_c) tau[my_n] = top_value(lane_value(top.entry, top_k - 1));
 }
 
@@ -469,8 +491,8 @@ void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t 
         if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
         else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
     };
-    // As many tokens a workgroup as leave every compute unit at most one. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 25.6 /
-    // 22.0 / 26.4 us, 2000 51 / 29 / 28, 8000 199 / 120 / 84.
+    // As many tokens a workgroup as leave every compute unit at most one. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 27.5 /
+    // 24.2 / 30.3 us, 2000 55 / 31 / 32, 8000 211 / 123 / 90.
     if (cv.n_c <= JOIN_ALONE) go(std::integral_constant<int, 1>{});
     else if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
     else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});

@@ -58,7 +58,7 @@ __device__ __forceinline__ uint64_t kth_of_lanes(float z, int k, int lane) {
 
 // Newcomers that beat the list's last entry gather in LDS (`pending`, of this wavefront) and are sorted and merged by 64, and what is left at
 // the end: some 10 instructions for 64 on offer and 250 a merge, against 20 for each that is inserted by itself.
-constexpr int PENDING = 128, PENDING4 = 320;     // keys of a buffer for lists that are offered one key a lane at a time, or four
+constexpr int PENDING = 128, PENDING4 = 320;     // keys of a buffer: up to 63 that wait, and one or four new ones a lane
 struct TopList {
     uint64_t* pending;
     int waiting = 0;
@@ -89,17 +89,11 @@ struct TopList {
             settle(k);
         }
     }
-    __device__ __forceinline__ void offer(uint64_t key, int k, int lane) {
-        add(key);
-        take(k, lane, 63);
-    }
     // The lane's logits x[0 .. 3] of indices v to v + 3, those below V.
-    __device__ __forceinline__ void offer4(const float (&x)[4], int v, int V, int k, int lane) {
+    __device__ __forceinline__ void add4(const float (&x)[4], int v, int V) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) add(v + q < V ? top_key(x[q], (uint32_t)(v + q)) : 0);
-        take(k, lane, 63);
     }
-    __device__ __forceinline__ void flush(int k, int lane) { take(k, lane, 0); }
     // Joins keys in descending order: the larger of each mirrored pair are the 64 largest, in bitonic order.
     __device__ __forceinline__ void merge(uint64_t sorted, int lane) {
         const uint64_t o = xor_lane<63>(sorted);
