@@ -152,6 +152,7 @@ def _ptr(t: Optional[torch.Tensor]):
 # The smallest calls are bound by what happens here before their launches. The raw handle of the current stream comes from
 # torch's own accessor (0.1 us; the Stream object of the public call takes 2.1 us, five times a step).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (without the checks of a first use)
 
 
 def _stream(device) -> int:
@@ -423,21 +424,19 @@ def _arg(t, name: str, dtype, shape: tuple, device):
     return t.data_ptr()
 
 
-class _on_device:
-    """Makes a tensor's device the current one for a call (the library launches on the current device)."""
+def _matrix(t, name: str):
+    """The address of a matrix that sets its own type, shape and device."""
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
 
-    def __init__(self, device):
-        if device.type != "cuda":
-            raise ValueError("the DPPO library takes device tensors only")
-        self.guard = torch.cuda.device(device) if torch.cuda.current_device() != device.index else None
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _elsewhere(t):
+    """None if t's device is the current one (the library launches on that), else the guard that makes it so."""
+    device = t.device
+    if not t.is_cuda:
+        raise ValueError("the DPPO library takes device tensors only")
+    return None if device.index == _get_device() else torch.cuda.device(device)
 
 
 def _stats_args(H, W, ids, loss_pos, status):
@@ -451,7 +450,7 @@ def _stats_args(H, W, ids, loss_pos, status):
     N = T
     if loss_pos is not None:
         N = loss_pos.numel()
-    ptrs = (_arg(H, "H", H.dtype, H.shape, device), _arg(W, "W", H.dtype, (V, D), device),
+    ptrs = (_matrix(H, "H"), _arg(W, "W", H.dtype, (V, D), device),
             _arg(ids, "ids", torch.int32, (T,), device), _arg(loss_pos, "loss_pos", torch.int32, (N,), device),
             _arg(status, "status", torch.int32, (1,), device))
     return HeadShape(T, N, D, V, code), ptrs
@@ -483,32 +482,35 @@ def dppo_token_stats(H, W, ids=None, loss_pos=None, top_k: int = 0, h_scale=None
     or None (no logp). Returns dict(logp[N] or None, lse[N], entropy[N], top_ids[N,top_k] and top_logp[N,top_k], None for
     top_k = 0) of device tensors; status: see dppo_token_logprob."""
     lib = _lib or load()
+    guard = _elsewhere(H)
+    if guard is not None:
+        with guard:
+            return dppo_token_stats(H, W, ids, loss_pos, top_k, h_scale, w_scale, ws, status)
     device = H.device
     shape, (H_, W_, ids_, loss_pos_, status_) = _stats_args(H, W, ids, loss_pos, status)
     N = shape.N
     scales = (_arg(h_scale, "h_scale", torch.float32, (shape.T,), device), _arg(w_scale, "w_scale", torch.float32, (shape.V,), device))
-    with _on_device(device):
-        ws = _stats_workspace(ws, shape, top_k, 0, device)
-        # one allocation for the results, each of which begins at a multiple of 16 bytes (4-byte words all of them)
-        room, k = N + 3 & -4, top_k if 0 < top_k <= TOP_K_MAX else 0
-        room_k = N * k + 3 & -4
-        buf = torch.empty(3 * room + 2 * room_k, dtype=torch.float32, device=device)
-        at = buf.data_ptr() if N else None
-        logp = top_ids = top_logp = None
-        if k:
-            lse, entropy, logp, top_logp, top_ids = _pieces(buf, [N] * 3 + [N * k] * 2, [room] * 3 + [room_k] * 2)
-            top_logp = top_logp.view(N, k)
-            top_ids = top_ids.view(torch.int32).view(N, k)
-        else:
-            lse, entropy, logp = _pieces(buf, [N] * 3, [room] * 3)
-        if ids is None:
-            logp = None
-        base = at or 0
-        st = lib.dppo_token_stats(shape, top_k, H_, W_, scales[0], scales[1], ids_, loss_pos_,
-                                  base + 8 * room if ids is not None else None, at, base + 4 * room,
-                                  base + 12 * room + 4 * room_k if k else None, base + 12 * room if k else None,
-                                  status_, ws.data_ptr(), ws.numel(), _stream(device))
-        _check(st, "dppo_token_stats")
+    ws = _stats_workspace(ws, shape, top_k, 0, device)
+    # one allocation for the results, each of which begins at a multiple of 16 bytes (4-byte words all of them)
+    room, k = N + 3 & -4, top_k if 0 < top_k <= TOP_K_MAX else 0
+    room_k = N * k + 3 & -4
+    buf = torch.empty(3 * room + 2 * room_k, dtype=torch.float32, device=device)
+    at = buf.data_ptr() if N else None
+    logp = top_ids = top_logp = None
+    if k:
+        lse, entropy, logp, top_logp, top_ids = _pieces(buf, [N] * 3 + [N * k] * 2, [room] * 3 + [room_k] * 2)
+        top_logp = top_logp.view(N, k)
+        top_ids = top_ids.view(torch.int32).view(N, k)
+    else:
+        lse, entropy, logp = _pieces(buf, [N] * 3, [room] * 3)
+    if ids is None:
+        logp = None
+    base = at or 0
+    st = lib.dppo_token_stats(shape, top_k, H_, W_, scales[0], scales[1], ids_, loss_pos_,
+                              base + 8 * room if ids is not None else None, at, base + 4 * room,
+                              base + 12 * room + 4 * room_k if k else None, base + 12 * room if k else None,
+                              status_, ws.data_ptr(), ws.numel(), _stream(device))
+    _check(st, "dppo_token_stats")
     return dict(logp=logp, lse=lse, entropy=entropy, top_ids=top_ids, top_logp=top_logp)
 
 
@@ -519,6 +521,10 @@ def dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy=None, g_logp=None, g_
     """Gradients of a loss given its derivatives by logp, lse and entropy ([N] float32 each or None), with lse and entropy as
     dppo_token_stats returned them. Returns dict(dH[T,D], dW[V,D] of dW_dtype or of the buffer handed in)."""
     lib = _lib or load()
+    guard = _elsewhere(H)
+    if guard is not None:
+        with guard:
+            return dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy, g_logp, g_lse, g_entropy, dH, dW, accumulate_dW, dW_dtype, ws, status)
     device = H.device
     shape, (H_, W_, ids_, loss_pos_, status_) = _stats_args(H, W, ids, loss_pos, status)
     if shape.dtype == 2:
@@ -534,16 +540,15 @@ def dppo_token_stats_bwd(H, W, ids, loss_pos, lse, entropy=None, g_logp=None, g_
     if dW_dtype is not torch.float32 and dW_dtype is not torch.bfloat16:
         raise ValueError("dW must be float32 or bfloat16")
     _arg(dH, "dH", H.dtype, H.shape, device)
-    with _on_device(device):
-        ws = _stats_workspace(ws, shape, 0, 2 if dW_dtype is torch.bfloat16 else 1, device)
-        if dH is None:
-            dH = torch.empty_like(H)
-        if dW is None:
-            dW = torch.empty(W.shape, dtype=dW_dtype, device=device)
-        p = StatsGradParams(1 if accumulate_dW else 0, _STATS_DTYPES[dW_dtype])
-        st = lib.dppo_token_stats_bwd(shape, p, H_, W_, ids_, loss_pos_, *per_token, dH.data_ptr(), dW.data_ptr(), status_,
-                                      ws.data_ptr(), ws.numel(), _stream(device))
-        _check(st, "dppo_token_stats_bwd")
+    ws = _stats_workspace(ws, shape, 0, 2 if dW_dtype is torch.bfloat16 else 1, device)
+    if dH is None:
+        dH = torch.empty_like(H)
+    if dW is None:
+        dW = torch.empty(W.shape, dtype=dW_dtype, device=device)
+    p = StatsGradParams(1 if accumulate_dW else 0, _STATS_DTYPES[dW_dtype])
+    st = lib.dppo_token_stats_bwd(shape, p, H_, W_, ids_, loss_pos_, *per_token, dH.data_ptr(), dW.data_ptr(), status_,
+                                  ws.data_ptr(), ws.numel(), _stream(device))
+    _check(st, "dppo_token_stats_bwd")
     return dict(dH=dH, dW=dW)
 
 
@@ -551,17 +556,20 @@ def dppo_quantize_rows(X: torch.Tensor):
     """X [rows, D] float32 or bfloat16 -> (q [rows, D rounded up to a multiple of 128] int8, padded with zeros,
     scale [rows] float32) with X ~ q[:, :D] * scale[:, None]."""
     lib = _lib or load()
+    guard = _elsewhere(X)
+    if guard is not None:
+        with guard:
+            return dppo_quantize_rows(X)
     code = _STATS_DTYPES.get(X.dtype, 2)
     if code == 2 or X.dim() != 2:
         raise ValueError("X must be a float32 or bfloat16 matrix")
     rows, D = X.shape
     device = X.device
-    X_ = _arg(X, "X", X.dtype, X.shape, device)
+    X_ = _matrix(X, "X")
     pitch = (D + I8_ROW - 1) // I8_ROW * I8_ROW
-    with _on_device(device):
-        q = torch.empty((rows, pitch), dtype=torch.int8, device=device)
-        scale = torch.empty(rows, dtype=torch.float32, device=device)
-        _check(lib.dppo_quantize_rows(rows, D, code, X_, q.data_ptr(), pitch, scale.data_ptr(), _stream(device)), "dppo_quantize_rows")
+    q = torch.empty((rows, pitch), dtype=torch.int8, device=device)
+    scale = torch.empty(rows, dtype=torch.float32, device=device)
+    _check(lib.dppo_quantize_rows(rows, D, code, X_, q.data_ptr(), pitch, scale.data_ptr(), _stream(device)), "dppo_quantize_rows")
     return q, scale
 
 
@@ -569,6 +577,10 @@ def dppo_matmul_i8(X, x_scale, W, w_scale, out_dtype: torch.dtype = torch.float3
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """X [T,D] int8 with x_scale [T], W [V,D] int8 with w_scale [V] -> Y [T,V] = X W^T * w_scale * x_scale, float32 or bfloat16."""
     lib = _lib or load()
+    guard = _elsewhere(X)
+    if guard is not None:
+        with guard:
+            return dppo_matmul_i8(X, x_scale, W, w_scale, out_dtype, out)
     device = X.device
     if X.dim() != 2 or W.dim() != 2:
         raise ValueError("X [T,D] and W [V,D] must be int8 matrices")
@@ -580,11 +592,10 @@ def dppo_matmul_i8(X, x_scale, W, w_scale, out_dtype: torch.dtype = torch.float3
         _arg(out, "out", out_dtype, (T, V), device)
     if out_dtype is not torch.float32 and out_dtype is not torch.bfloat16:
         raise ValueError("the result is float32 or bfloat16")
-    with _on_device(device):
-        if out is None:
-            out = torch.empty((T, V), dtype=out_dtype, device=device)
-        _check(lib.dppo_matmul_i8(T, V, D, X_, xs_, W_, ws_, out.data_ptr(), _STATS_DTYPES[out_dtype], _stream(device)),
-               "dppo_matmul_i8")
+    if out is None:
+        out = torch.empty((T, V), dtype=out_dtype, device=device)
+    _check(lib.dppo_matmul_i8(T, V, D, X_, xs_, W_, ws_, out.data_ptr(), _STATS_DTYPES[out_dtype], _stream(device)),
+           "dppo_matmul_i8")
     return out
 
 
