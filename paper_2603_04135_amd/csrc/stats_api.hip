@@ -292,22 +292,24 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
         const ChunkView cv = view(n0, s.N, r.n_cp);
         // dW sums over the chunk's tokens up to whole slices of its GEMM
         const int32_t n_sum = round_up32(cv.n_c, GEMM_B_BLOCK_K);
-        {
+        const GatherRows rows{tokens, r.row_bytes, nullptr, r.small ? nullptr : Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
+                              n0 == 0 ? (size_t)s.T * r.row_bytes : 0, s.dtype == BF16 ? w + r.o_hct : nullptr, n_sum,
+                              r.small ? SMALL_BLOCK_ROWS : GEMM_B_BLOCK_ROWS};
+        if (s.dtype == BF16) {
             StageTimer tm(DPPO_STAGE_ELEMENTWISE, st);
-            launch_stats_gather(GatherRows{tokens, r.row_bytes, nullptr, r.small ? nullptr : Hc, y, rowc, nullptr, n0 == 0 ? dH : nullptr,
-                                           n0 == 0 ? (size_t)s.T * r.row_bytes : 0, s.dtype == BF16 ? w + r.o_hct : nullptr, n_sum,
-                                           r.small ? SMALL_BLOCK_ROWS : GEMM_B_BLOCK_ROWS}, cv, st);
+            launch_stats_gather(rows, cv, st);
         }
         StoreSpec oh{loss_pos ? dH : reinterpret_cast<char*>(dH) + (size_t)n0 * r.row_bytes, s.D, 0, loss_pos ? rowc : nullptr};
         StoreSpec ow{dw_sum, s.D, n0 == 0 && !p->accumulate_dW ? 0 : 1, nullptr};
         if (s.dtype == F32) {
             const float* Hf = reinterpret_cast<const float*>(Hc);
             float* Gf = reinterpret_cast<float*>(G);
-            launch_gemm_f32(GemmF32{Hf, s.D, 0, reinterpret_cast<const float*>(W), s.D, 0, cv.n_c, s.V, s.D, Gf, r.Vp, 0, nullptr, nullptr, 0,
-                                    nullptr, 0}, cus, st);
+            const float* A = reinterpret_cast<const float*>(H) + (loss_pos ? 0 : (size_t)n0 * s.D);
+            launch_gemm_f32(GemmF32{A, s.D, 0, reinterpret_cast<const float*>(W), s.D, 0, cv.n_c, s.V, s.D, Gf, r.Vp, 0, nullptr, nullptr, 0,
+                                    loss_pos ? loss_pos + n0 : nullptr, (int32_t)s.T}, cus, st);
             {
                 StageTimer tm(DPPO_STAGE_GRAD_LOGITS, st);
-                launch_stats_grad_f32(Gf, s.V, r.Vp, y, grad, cv, st);
+                launch_stats_grad_f32(Gf, r.Vp, grad, rows, cv, st);
             }
             launch_gemm_f32(GemmF32{Gf, r.Vp, 0, reinterpret_cast<const float*>(W), s.D, 1, cv.n_c, s.D, s.V, reinterpret_cast<float*>(oh.C),
                                     oh.ldc, 0, oh.row_map, r.f32_parts > 1 ? reinterpret_cast<float*>(w + r.o_fpart) : nullptr,

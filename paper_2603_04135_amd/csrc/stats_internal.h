@@ -89,7 +89,8 @@ __device__ __forceinline__ float grad_entry(const TokenGrad& t, float lp, float 
     const float cut = fmaxf(lp, -150.0f);
     return target ? fmaf(t.gl, 1.0f - p, p * (t.gs - t.ge * (cut + t.ent))) : p * fmaf(-t.ge, cut, t.c);
 }
-void launch_stats_grad_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const StatsGrad& g, ChunkView cv, hipStream_t st);
+// float32 entries in place over the stored logits, and the gathering beside them (no transpose).
+void launch_stats_grad_f32(float* ZG, int32_t Vp, const StatsGrad& g, const GatherRows& rows, ChunkView cv, hipStream_t st);
 // dst (bfloat16) = src, n a multiple of 4, both 16-byte aligned.
 void launch_to_bf16(const float* src, void* dst, size_t n, hipStream_t st);
 

@@ -378,25 +378,26 @@ __device__ void transpose_tokens(const GatherRows& g, ChunkView cv, int block, u
         *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.transpose) + off) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
-__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv, unsigned gather_blocks, unsigned transpose_blocks) {
-    __shared__ uint16_t tile[64][64 + 2];
-    if (blockIdx.x >= gather_blocks + transpose_blocks) {
+// Workgroup `block` of `blocks`.
+struct GatherBlocks { unsigned gather, transpose, all; };
+__device__ __forceinline__ void gather_rows(const GatherRows& g, ChunkView cv, unsigned block, const GatherBlocks& blocks, uint16_t (*tile)[64 + 2]) {
+    if (block >= blocks.gather + blocks.transpose) {
         // (clear is 4-byte aligned, the words in front of and behind the vectors one by one)
         uint32_t* p = reinterpret_cast<uint32_t*>(g.clear);
-        const unsigned first = gather_blocks + transpose_blocks;
+        const unsigned first = blocks.gather + blocks.transpose;
         const size_t words = g.clear_bytes / 4, head = (size_t)(-(reinterpret_cast<intptr_t>(p) / 4) & 3), lead = head < words ? head : words;
-        const size_t vectors = (words - lead) / 4, i0 = (size_t)(blockIdx.x - first) * 256 + threadIdx.x;
+        const size_t vectors = (words - lead) / 4, i0 = (size_t)(block - first) * 256 + threadIdx.x;
         uint4* v = reinterpret_cast<uint4*>(p + lead);
-        for (size_t i = i0; i < vectors; i += (size_t)(gridDim.x - first) * 256) v[i] = make_uint4(0, 0, 0, 0);
+        for (size_t i = i0; i < vectors; i += (size_t)(blocks.all - first) * 256) v[i] = make_uint4(0, 0, 0, 0);
         if (i0 < lead) p[i0] = 0;
         if (lead + vectors * 4 + i0 < words) p[lead + vectors * 4 + i0] = 0;
         return;
     }
-    if (blockIdx.x >= gather_blocks) {
-        transpose_tokens(g, cv, (int)(blockIdx.x - gather_blocks), tile);
+    if (block >= blocks.gather) {
+        transpose_tokens(g, cv, (int)(block - blocks.gather), tile);
         return;
     }
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int n = (int)block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
     if (n >= cv.n_cp) return;
     const bool valid = n < cv.n_c;
     int64_t row = 0;
@@ -442,16 +443,31 @@ __global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkVi
     }
 }
 
+__global__ __launch_bounds__(256) void stats_gather_kernel(GatherRows g, ChunkView cv, GatherBlocks blocks) {
+    __shared__ uint16_t tile[64][64 + 2];
+    gather_rows(g, cv, blockIdx.x, blocks, tile);
+}
+
 // Gradient entries of the float32 path, in place over the stored logits: dz = p (c - g_ent (z - lse)) with
-// c = g_lse - g_logp - g_ent entropy, the target's g_logp (1 - p) + p (g_lse - g_ent (z - lse + entropy)); 0 for V <= v < Vp.
-__global__ __launch_bounds__(256) void stats_grad_kernel(float* __restrict__ ZG, int32_t V, int32_t Vp, const int32_t* __restrict__ y,
-                                                         StatsGrad g, ChunkView cv) {
-    const int n = blockIdx.x;
+// c = g_lse - g_logp - g_ent entropy, the target's g_logp (1 - p) + p (g_lse - g_ent (z - lse + entropy)); 0 for V <= v < Vp. `parts` workgroups a
+// token; those behind them gather what the two GEMMs after this need (a launch of its own costs the host 3 us).
+__global__ __launch_bounds__(256) void stats_grad_kernel(float* __restrict__ ZG, int32_t V, int32_t Vp, StatsGrad g, ChunkView cv, unsigned parts,
+                                                         GatherRows rows, GatherBlocks blocks) {
+    const unsigned entries = (unsigned)cv.n_c * parts;
+    if (blockIdx.x >= entries) {
+        gather_rows(rows, cv, blockIdx.x - entries, blocks, nullptr);
+        return;
+    }
+    const int n = (int)(blockIdx.x / parts), part = (int)(blockIdx.x % parts);
     const TokenGrad t = load_grad(g, cv.n0 + n);
-    const int target = y[n];
-    float4* row = reinterpret_cast<float4*>(ZG + (size_t)n * Vp);
-    for (int i = blockIdx.y * 256 + threadIdx.x; i < Vp / 4; i += gridDim.y * 256) {
-        const float4 z = row[i];
+    int32_t target = -1;
+    if (rows.tokens.ids) {
+        int64_t row;
+        locate_token(rows.tokens.ids, rows.tokens.loss_pos, rows.tokens.T, rows.tokens.V, cv.n0 + n, row, target);
+    }
+    float4* z4 = reinterpret_cast<float4*>(ZG + (size_t)n * Vp);
+    for (int i = part * 256 + threadIdx.x; i < Vp / 4; i += parts * 256) {
+        const float4 z = z4[i];
         const float zz[4] = {z.x, z.y, z.z, z.w};
         float d[4];
 #pragma unroll
@@ -460,7 +476,7 @@ __global__ __launch_bounds__(256) void stats_grad_kernel(float* __restrict__ ZG,
             const float lp = zz[q] - t.lse;
             d[q] = v < V ? grad_entry(t, lp, expf(lp), v == target) : 0.0f;
         }
-        row[i] = make_float4(d[0], d[1], d[2], d[3]);
+        z4[i] = make_float4(d[0], d[1], d[2], d[3]);
     }
 }
 
@@ -512,17 +528,25 @@ void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, Ch
     stats_bound_kernel<<<(unsigned)ceil_div(cv.n_c, BOUND_TOK), 1024, 0, st>>>(part, groups, top_k, cv.n_c, tau);
 }
 
-void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {
-    const unsigned blocks = (unsigned)ceil_div(cv.n_cp, 4);
-    const unsigned transposes = g.transpose ? (unsigned)(g.tokens.D / 64 * (g.transpose_cols / 64)) : 0;
+static GatherBlocks gather_blocks(const GatherRows& g, ChunkView cv) {
+    GatherBlocks b;
+    b.gather = (unsigned)ceil_div(cv.n_cp, 4);
+    b.transpose = g.transpose ? (unsigned)(g.tokens.D / 64 * (g.transpose_cols / 64)) : 0;
     const int64_t fill = ceil_div((int64_t)g.clear_bytes, 16 * 256 * 4);
-    stats_gather_kernel<<<blocks + transposes + (unsigned)(fill < 4096 ? fill : 4096), 256, 0, st>>>(g, cv, blocks, transposes);
+    b.all = b.gather + b.transpose + (unsigned)(fill < 4096 ? fill : 4096);
+    return b;
 }
 
-void launch_stats_grad_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const StatsGrad& g, ChunkView cv, hipStream_t st) {
-    int by = (int)ceil_div(Vp / 4, 256);
-    if (by > 64) by = 64;
-    stats_grad_kernel<<<dim3((unsigned)cv.n_c, (unsigned)by), 256, 0, st>>>(ZG, V, Vp, y, g, cv);
+void launch_stats_gather(const GatherRows& g, ChunkView cv, hipStream_t st) {
+    const GatherBlocks b = gather_blocks(g, cv);
+    stats_gather_kernel<<<b.all, 256, 0, st>>>(g, cv, b);
+}
+
+void launch_stats_grad_f32(float* ZG, int32_t Vp, const StatsGrad& g, const GatherRows& rows, ChunkView cv, hipStream_t st) {
+    const GatherBlocks b = gather_blocks(rows, cv);
+    int parts = (int)ceil_div(Vp / 4, 256);
+    if (parts > 64) parts = 64;
+    stats_grad_kernel<<<(unsigned)cv.n_c * (unsigned)parts + b.all, 256, 0, st>>>(ZG, rows.tokens.V, Vp, g, cv, (unsigned)parts, rows, b);
 }
 
 void launch_to_bf16(const float* src, void* dst, size_t n, hipStream_t st) {
