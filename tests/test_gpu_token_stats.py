@@ -760,3 +760,14 @@ def test_gradient_of_every_tile(P, N, D, V, positions):
         first = r
     dW0 = torch.randn(c.W.shape, device=DEV)
     check_grads(c, g, backward(P, c, g, dW=dW0.clone(), accumulate_dW=True), dW0)
+
+
+@pytest.mark.parametrize("dtype,N,D,V,k", [("bf16", 384, 64, 100001, 20), ("bf16", 384, 64, 100001, 1), ("i8", 384, 128, 100001, 5),
+                                           ("bf16", 1100, 64, 60001, 64), ("bf16", 250, 64, 151936, 20), ("bf16", 1501, 64, 70001, 20),
+                                           ("i8", 1025, 128, 40001, 3)])
+def test_statistics_of_leading_tiles_and_columns_of_192(P, dtype, N, D, V, k):
+    """Sizes at which the bound from leading tiles keeps logits from being stored, with either width of columns."""
+    c = Case(dtype, N, D, V, seed=40)
+    out = c.call(P, k)
+    _, y = c.rows()
+    check_stats(out, c.logits(), y, k)
