@@ -491,24 +491,24 @@ def dppo_token_stats(H, W, ids=None, loss_pos=None, top_k: int = 0, h_scale=None
     N = shape.N
     scales = (_arg(h_scale, "h_scale", torch.float32, (shape.T,), device), _arg(w_scale, "w_scale", torch.float32, (shape.V,), device))
     ws = _stats_workspace(ws, shape, top_k, 0, device)
-    # one allocation for the results, each of which begins at a multiple of 16 bytes (4-byte words all of them)
-    room, k = N + 3 & -4, top_k if 0 < top_k <= TOP_K_MAX else 0
-    room_k = N * k + 3 & -4
-    buf = torch.empty(3 * room + 2 * room_k, dtype=torch.float32, device=device)
+    # one allocation for the results, side by side (4-byte words all of them; the library asks for no more of their addresses)
+    k = top_k if 0 < top_k <= TOP_K_MAX else 0
+    sizes = [N] * 3 + [N * k] * 2 if k else [N] * 3
+    buf = torch.empty(3 * N + 2 * N * k, dtype=torch.float32, device=device)
     at = buf.data_ptr() if N else None
     logp = top_ids = top_logp = None
     if k:
-        lse, entropy, logp, top_logp, top_ids = _pieces(buf, [N] * 3 + [N * k] * 2, [room] * 3 + [room_k] * 2)
+        lse, entropy, logp, top_logp, top_ids = _pieces(buf, sizes, sizes)
         top_logp = top_logp.view(N, k)
         top_ids = top_ids.view(torch.int32).view(N, k)
     else:
-        lse, entropy, logp = _pieces(buf, [N] * 3, [room] * 3)
+        lse, entropy, logp = _pieces(buf, sizes, sizes)
     if ids is None:
         logp = None
     base = at or 0
     st = lib.dppo_token_stats(shape, top_k, H_, W_, scales[0], scales[1], ids_, loss_pos_,
-                              base + 8 * room if ids is not None else None, at, base + 4 * room,
-                              base + 12 * room + 4 * room_k if k else None, base + 12 * room if k else None,
+                              base + 8 * N if ids is not None else None, at, base + 4 * N,
+                              base + 12 * N + 4 * N * k if k else None, base + 12 * N if k else None,
                               status_, ws.data_ptr(), ws.numel(), _stream(device))
     _check(st, "dppo_token_stats")
     return dict(logp=logp, lse=lse, entropy=entropy, top_ids=top_ids, top_logp=top_logp)
