@@ -285,7 +285,7 @@ int dppo_loss_fwd_bwd(const dppo_head_shape* shape, const dppo_loss_params* p, i
  * the same head in 8-bit integers.
  *
  * Arguments as in the section above, with these additions.
- *   dtype 2 (dppo_token_stats only): H and W are int8 rows of D bytes, D a multiple of 128 and at most 131072
+ *   dtype 2 (dppo_token_stats only): H and W are int8 rows of D bytes, D a multiple of 128 and at most 130944
  *     (dppo_quantize_rows pads rows with zeros); h_scale[T] and w_scale[V] are their scales, NULL for the other types.
  *     z[n, v] = (float)(exact integer sum) * w_scale[v] * h_scale[row], rounded to float32 after each step.
  *   ids may be NULL where no target is needed (no logp, no g_logp): a loss_pos entry is then valid in all of [0, T).
@@ -344,7 +344,7 @@ int dppo_quantize_rows(int64_t rows, int32_t D, int32_t dtype, const void* X,
 
 /* dppo_matmul_i8 -- Y[T, V] = X W^T of int8 rows with their scales (as dtype 2 above): the logits of a quantised head for a
  * sampler, or any linear layer. Integer sums are exact; out_dtype 0: float32, 1: bfloat16 (rounded once from the float32 value).
- * X[T, D] and W[V, D] 16-byte aligned, D a multiple of 128 of at most 131072; Y row-major with pitch V. */
+ * X[T, D] and W[V, D] 16-byte aligned, D a multiple of 128 of at most 130944; Y row-major with pitch V. */
 int dppo_matmul_i8(int64_t T, int32_t V, int32_t D, const int8_t* X, const float* x_scale,
                    const int8_t* W, const float* w_scale, void* Y, int32_t out_dtype, void* stream);
 

@@ -9,7 +9,7 @@ namespace {
 
 enum { F32 = 0, BF16 = 1, I8 = 2 };
 constexpr int32_t I8_ROW = 128;             // 8-bit rows are whole GEMM slices
-constexpr int32_t I8_D_MAX = 131072;        // 127 * 127 * D stays below 2^31
+constexpr int32_t I8_D_MAX = 130944;        // 128 * 128 * D stays below 2^31 (-128 is no result of quantisation, but a value)
 constexpr int32_t V_MAX = 1 << 30;
 // Stored logits of a forward chunk.
 constexpr size_t LOGITS_CHUNK_BYTES = (size_t)8 << 30;

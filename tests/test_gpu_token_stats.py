@@ -771,3 +771,13 @@ def test_statistics_of_leading_tiles_and_columns_of_192(P, dtype, N, D, V, k):
     out = c.call(P, k)
     _, y = c.rows()
     check_stats(out, c.logits(), y, k)
+
+
+@pytest.mark.parametrize("T,D,V", [(3, 256, 70), (40, 384, 300), (300, 128, 1000), (2, 130944, 5)])
+def test_matmul_i8_of_the_lowest_value(P, T, D, V):
+    """-128 everywhere: the largest sums there are."""
+    X, W = (torch.full((n, D), -128, dtype=torch.int8, device=DEV) for n in (T, V))
+    W[0] = 127
+    xs, ws = torch.ones(T, device=DEV), torch.ones(V, device=DEV)
+    Y = P.dppo_matmul_i8(X, xs, W, ws)
+    assert (Y[:, 1:] == 16384.0 * D).all() and (Y[:, 0] == float(np.float32(-128.0 * 127.0 * D))).all()

@@ -144,3 +144,11 @@ def test_formula_of_the_gradient_against_differences():
             e = np.zeros(V)
             e[v] = h
             assert abs((loss(z + e) - loss(z - e)) / (2 * h) - dz[v]) <= 1e-8
+
+
+def test_longest_int8_rows(lib):
+    """Sums of D products of -128 by -128 have to stay below 2^31."""
+    drop = ("top_ids", "top_logp")
+    assert 128 * 128 * 130944 < 2**31 <= 128 * 128 * 131072
+    assert stats(lib, (100, 50, 131072, 1000, 2), drop=drop) == 5
+    assert stats(lib, (100, 50, 130944, 1000, 2), drop=drop, ws_bytes=1000) == 4           # (accepted, but for the workspace)
