@@ -781,3 +781,27 @@ def test_matmul_i8_of_the_lowest_value(P, T, D, V):
     xs, ws = torch.ones(T, device=DEV), torch.ones(V, device=DEV)
     Y = P.dppo_matmul_i8(X, xs, W, ws)
     assert (Y[:, 1:] == 16384.0 * D).all() and (Y[:, 0] == float(np.float32(-128.0 * 127.0 * D))).all()
+
+
+@pytest.mark.parametrize("N", [3, 20, 300])
+def test_matrices_of_more_than_4_GiB(P, N):
+    """Byte offsets past 32 bits in W, in the result and in dW: the last rows are found, and nothing else."""
+    D = 4096
+    V = 1_200_011
+    X, W = torch.ones((N, D), dtype=torch.int8, device=DEV), torch.zeros((V, D), dtype=torch.int8, device=DEV)
+    W[-1], W[V // 2] = 1, 2
+    Y = P.dppo_matmul_i8(X, torch.ones(N, device=DEV), W, torch.ones(V, device=DEV))
+    assert (Y[:, -1] == D).all() and (Y[:, V // 2] == 2 * D).all() and (Y.count_nonzero(dim=1) == 2).all()
+    del X, W, Y
+    V = 600_011
+    H, W = torch.full((N, D), 1 / 64, dtype=torch.bfloat16, device=DEV), torch.zeros((V, D), dtype=torch.bfloat16, device=DEV)
+    W[-1] = 1
+    ids = torch.full((N,), V - 1, dtype=torch.int32, device=DEV)
+    f = P.dppo_token_stats(H, W, ids, None, top_k=3)
+    want = np.log(np.exp(64.0) + V - 1)
+    assert (f["top_ids"] == torch.tensor([V - 1, 0, 1], device=DEV, dtype=torch.int32)).all()
+    assert ((f["lse"].double() - want).abs() <= 4 * U32 * want).all() and (f["logp"].abs() <= 4 * U32 * want).all()
+    g = torch.ones(N, device=DEV)
+    b = P.dppo_token_stats_bwd(H, W, ids, None, f["lse"], g_lse=g, dW_dtype=torch.bfloat16)
+    assert ((b["dH"].float() - 1).abs() <= 0.01).all() and ((b["dW"][-1].float() - N / 64).abs() <= 0.01 * N / 64).all()
+    assert b["dW"][:-1].abs().max() <= 1e-20
