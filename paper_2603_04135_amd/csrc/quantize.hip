@@ -141,7 +141,13 @@ template <class E>
 void launch(const E* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float* scale, hipStream_t st) {
     auto go = [&](auto nv, auto wpr) {
         constexpr int WPR = decltype(wpr)::value;
-        quantize_rows_kernel<E, decltype(nv)::value, WPR><<<(unsigned)ceil_div(rows, 4 / WPR), 256, 0, st>>>(X, rows, D, q, pitch, scale);
+        // (a launch of 2^32 threads or more runs what is left of their number in 32 bits, and reports nothing)
+        constexpr int64_t MOST = (int64_t)(1 << 23) * (4 / WPR);
+        for (int64_t r0 = 0; r0 < rows; r0 += MOST) {
+            const int64_t n = rows - r0 < MOST ? rows - r0 : MOST;
+            quantize_rows_kernel<E, decltype(nv)::value, WPR><<<(unsigned)ceil_div(n, 4 / WPR), 256, 0, st>>>(
+                X + (size_t)r0 * D, n, D, q + (size_t)r0 * pitch, pitch, scale + r0);
+        }
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 4> four;

@@ -805,3 +805,15 @@ def test_matrices_of_more_than_4_GiB(P, N):
     b = P.dppo_token_stats_bwd(H, W, ids, None, f["lse"], g_lse=g, dW_dtype=torch.bfloat16)
     assert ((b["dH"].float() - 1).abs() <= 0.01).all() and ((b["dW"][-1].float() - N / 64).abs() <= 0.01 * N / 64).all()
     assert b["dW"][:-1].abs().max() <= 1e-20
+
+
+def test_quantize_more_rows_than_a_launch_has_threads_for(P):
+    """2^26 rows by four rows a workgroup of 256 threads are 2^32 threads: the rows go in ranges, and every one is answered."""
+    rows = 2 ** 26 + 2 ** 25 + 3
+    x = (torch.arange(rows, device=DEV, dtype=torch.int32) % 251 - 125).to(torch.bfloat16)[:, None]
+    q, scale = P.dppo_quantize_rows(x)
+    assert torch.equal(scale, x[:, 0].float().abs() * (np.float32(1) / np.float32(127)))
+    assert torch.equal(q[:, 0], x[:, 0].sign().mul(127).to(torch.int8))
+    words = q.view(torch.int64)                  # (a row's first word holds its one value, the other fifteen nothing)
+    assert torch.equal(words[:, 0] & 255, q[:, 0].to(torch.int64) & 255) and (words[:, 0] >> 8 == 0).all()
+    assert words[:, 1:].count_nonzero() == 0
