@@ -415,12 +415,7 @@ struct EpiStatsGradBoth {
 }  // namespace mfma
 
 namespace {
-// Tiles of 128 x 128 by eight wavefronts instead of four where no more than one workgroup runs on a compute unit (the reads of four from LDS show),
-// or few slices leave prologue and statistics most of the time. D = 512, statistics, four / eight: V = 5000, 128 tokens (40 tiles) 8.3 / 6.7 us
-// (8-bit product), V = 32000 (250) 12.4 / 10.8, 256 tokens (500) 15.1 / 14.4; D = 2560, V = 151936, 128 tokens 188 / 208; 8-bit product D = 4096,
-// V = 32000: 128 tokens (250) 28.1 / 26.3, 256 (500) 37 / 42.
-typedef PipeCfg<128, 128, 2, 4, 2, 1, 1> Cfg128Eight;
-inline bool eight_wavefronts(int32_t n, int32_t V, int32_t k2) { return ceil_div(V, 128) * ceil_div(n, 128) <= 256 || k2 <= 512; }
+typedef PipeCfg<128, 128, 2, 4, 2, 1, 1> Cfg128Eight;       // (see eight_wavefronts)
 template <class Epi>
 void launch_logits(const LogitsOut& g, const Epi& e, hipStream_t st, int first = 0, int count = -1) {
     auto mapped = [&](auto cfg) {

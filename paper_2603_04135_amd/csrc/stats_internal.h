@@ -2,6 +2,7 @@
 #pragma once
 #include "dppo_internal.h"
 #include "lanes.h"
+#include "stats_plan.h"
 
 namespace dppo {
 
@@ -44,7 +45,7 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
 // Statistics of the vocabulary GEMM by groups of rows, STATS_GROUPS of a tile (a unit of the kernel for few tokens is one): mx[at(g, n)]
 // is group g's maximum for token n, sd[at(g, n)] = {sum, dev} against it; zy[n]: target logits (or NULL). A token's groups lie side by side
 // up to JOIN_ALONE tokens, which a workgroup each joins, beyond that the tokens of a group.
-constexpr int STATS_GROUPS = 2, JOIN_ALONE = 256;
+constexpr int JOIN_ALONE = 256;
 struct StatsPart {
     float* mx; float2* sd; float* zy; int32_t group_step, token_step;
     __device__ __forceinline__ size_t at(int g, int n) const { return (size_t)g * group_step + (size_t)n * token_step; }
@@ -99,37 +100,6 @@ void launch_to_bf16(const float* src, void* dst, size_t n, hipStream_t st);
 struct OperandScales {
     const float* w; const float* h; const int32_t* map; int32_t rows;
 };
-// Tile of the vocabulary GEMM, rows (vocabulary) x columns (tokens); FEW: the kernel for few tokens. All but the largest read the tokens' rows
-// of H through a map.
-enum LogitsTile { TILE_FEW = 0, TILE_128x96 = 1, TILE_128x128 = 2, TILE_256x192 = 3, TILE_256x256 = 4 };
-constexpr int32_t FEW_TILE_TOKENS = 16, FEW_TILE_ROWS = 32, FEW_ROW_BYTES_BF16 = 8192, FEW_ROW_BYTES_I8 = 6144;
-inline int32_t tile_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile <= TILE_128x128 ? 128 : 256; }
-// Rows of a group of a tile (see StatsPart).
-inline int32_t group_rows(int tile) { return tile == TILE_FEW ? FEW_TILE_ROWS : tile_rows(tile) / STATS_GROUPS; }
-// Groups of all tiles (the last may lie behind the vocabulary).
-inline int32_t groups_of_tiles(int tile, int32_t V) { return (int32_t)ceil_div(V, tile_rows(tile)) * (tile == TILE_FEW ? 1 : STATS_GROUPS); }
-// For n tokens with operand rows of 2 k2 bytes. Up to 16 tokens: rows of up to 8 KB (8-bit operands 6 KB) are what the registers of the
-// kernel for few tokens hold. Up to 128 tokens as for the log-probabilities alone (see CfgFew; by 128 columns where every tile has a compute
-// unit to itself). Beyond, the tile whose rounds of the chip
-// take the least time, 256 x 256 : 256 x 192 : two of 128 x 128 as 20 : 18 : 15, the last while large tiles fill no more than two rounds.
-// Statistics, 256 x 256 / 256 x 192 / 128 x 128, with the rounds of each: D = 1024, V = 32000: 224 tokens (1/1/1) 30 / 29 / 22 us, 384
-// (1/1/2) 34 / 29 / 34, 512 (1/2/2) 35 / 44 / 37, 576 (2/2/3) 54 / 44 / 48, 768 (2/2/3) 55 / 48 / 52, 1024 (2/3/4) 61 / 72 / 72, 1152
-// (3/3/5) 82 / 70 / 80; D = 4096, V = 60000: 224 (1/2/2) 144 / 163 / 157, 576 (3/3/5) 255 / 233 / 294, 1152 (5/6/9) 430 / 435 / 523;
-// D = 2560, V = 151936: 192 (3/3/10) 216 / 201 / 244, 384 (5/5/14) 297 / 287 / 335, 640 (7/10/-) 423 / 496 / 530.
-constexpr int64_t SMALL_TILES_MOST = 512;
-inline int logits_tile(int32_t n, int32_t V, int32_t k2, bool i8) {
-    if (n <= FEW_TILE_TOKENS && 2 * k2 <= (i8 ? FEW_ROW_BYTES_I8 : FEW_ROW_BYTES_BF16)) return TILE_FEW;
-    constexpr int64_t CHIP = 256;                 // compute units
-    if (n <= 96 && ceil_div(V, 128) > CHIP) return TILE_128x96;
-    if (n <= 128) return TILE_128x128;
-    const int64_t rows = ceil_div(V, 256), large = rows * ceil_div(n, 256);
-    const int64_t t256 = 20 * ceil_div(large, CHIP), t192 = 18 * ceil_div(rows * ceil_div(n, 192), CHIP);
-    const int64_t t128 = 15 * ceil_div(ceil_div(V, 128) * ceil_div(n, 128), 2 * CHIP);
-    if (large <= SMALL_TILES_MOST && t128 < t256 && t128 < t192) return TILE_128x128;
-    return t192 < t256 ? TILE_256x192 : TILE_256x256;
-}
-// Most pairs of (tile, token) that 128 x 128 tiles beyond 128 tokens make.
-constexpr size_t SMALL_TILE_PAIRS = 2 * SMALL_TILES_MOST * 256;
 // Logits of n tokens, C[n, V] = H W^T with pitch ldc, by tiles of the given kind. k2: bytes of an operand row / 2 (a multiple of 64). Row n
 // of the tokens is row map[n] (clamped to h_rows) of H, or n where map is NULL, as it has to be for the largest tile.
 struct LogitsOut {
@@ -156,35 +126,17 @@ void launch_mfma_stats_grad(const void* W, int32_t V, int32_t D, const void* Hc,
 // launch_mfma_dw with a bfloat16 result, overwritten.
 void launch_mfma_dw_bf16(int cus, const void* G, int32_t Vp, const void* HcT, int32_t n_cp, int32_t V, int32_t D, void* dW, float* partial,
                          hipStream_t st);
-// The gradient by tiles of 128 x 128, for problems that large ones leave much of the chip idle in: the entries row-major both ways, G[n_c, Vk]
-// and GT[V, n_sum] (Vk, n_sum: V, n_c up to multiples of 64, zero there), H's rows through a map. HT: see GatherRows::transpose, by blocks of
-// 128. One chunk, no more than a chip of large tiles of entries, and of dW few (or next to no sum to each). Large tiles / these: D = 512,
-// V = 5000: 60 tokens 44 / 30 us, 1000 80 / 58; D = 2560, V = 3000: 60 68 / 52, 2500 193 / 149; D = 256, V = 20000: 300 68 / 52; D = 1024, V =
-// 12000 (188 large tiles of dW): 600 99 / 84, 750 104 / 107; V = 32000 (500): 60 77 / 74, 500 135 / 150.
+// The gradient by tiles of 128 x 128 (see small_grad): the entries row-major both ways, G[n_c, Vk] and GT[V, n_sum] (Vk, n_sum: V, n_c up to
+// multiples of 64, zero there), H's rows through a map. HT: see GatherRows::transpose, by blocks of 128.
 struct SmallGrad {
     const void* W; int32_t V, D;
     const void* H; int64_t h_rows; const int32_t* map; ChunkView cv; int32_t n_sum, Vk;
     void* G; void* GT; const void* HT; float* partial;
 };
 constexpr int32_t SMALL_BLOCK_ROWS = 128;
-inline bool small_grad(int64_t N, int32_t D, int32_t V) {
-    return ceil_div(V, 256) * ceil_div(N, 256) <= 256 && (N <= 64 || ceil_div(V, 256) * ceil_div(D, 256) <= 192);
-}
 void launch_small_grad(const SmallGrad& s, const int32_t* y, const StatsGrad& g, hipStream_t st);
 void launch_small_dh(const SmallGrad& s, const StoreSpec& out, int cus, hipStream_t st);
 void launch_small_dw(const SmallGrad& s, const StoreSpec& out, bool bf16, int cus, hipStream_t st);
-// Parts along K of a GEMM of few tiles of 128 x 128: least estimated time of a slice's 0.45 us, 0.033 a partial tile (64 KB written and
-// read) and 4 for the launch that sums them. Two workgroups a compute unit, 4 slices or more each; 64 MB of partial tiles at most.
-inline int small_tiles_parts(int cus, int tiles, int slices) {
-    const int slots = 2 * (cus < 256 ? cus : 256);
-    int best = 1;
-    double best_t = 0.45 * slices * (double)((tiles + slots - 1) / slots);
-    for (int p = 2; p <= slices / 4 && tiles * p <= slots; ++p) {
-        const double t = 0.45 * ((slices + p - 1) / p) + 4.0 + 0.033 * tiles * p;
-        if (t < best_t) { best_t = t; best = p; }
-    }
-    return best;
-}
 
 // ---- 8-bit rows (quantize.hip) -------------------------------------------------
 void launch_quantize_rows(int dtype, const void* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float* scale, hipStream_t st);
