@@ -44,7 +44,10 @@ constexpr size_t SMALL_TILE_PAIRS = 2 * SMALL_TILES_MOST * 256;
 // or few slices leave prologue and statistics most of the time. D = 512, statistics, four / eight: V = 5000, 128 tokens (40 tiles) 8.3 / 6.7 us
 // (8-bit product), V = 32000 (250) 12.4 / 10.8, 256 tokens (500) 15.1 / 14.4; D = 2560, V = 151936, 128 tokens 188 / 208; 8-bit product D = 4096,
 // V = 32000: 128 tokens (250) 28.1 / 26.3, 256 (500) 37 / 42.
-inline bool eight_wavefronts(int32_t n, int32_t V, int32_t k2) { return div_up(V, 128) * div_up(n, 128) <= 256 || k2 <= 512; }
+inline bool eight_wavefronts(int32_t n, int32_t V, int32_t k2) {
+    const int64_t tiles = div_up(V, 128) * div_up(n, 128);
+    return tiles <= 256 || (k2 <= 512 && tiles < (int64_t)1 << 23);       // (2^23 tiles of 512 threads are more than a launch has)
+}
 
 // Whether the gradient goes by tiles of 128 x 128 (see SmallGrad): problems that large ones leave much of the chip idle in. One chunk, no more than a
 // chip of large tiles of entries, and of dW few (or next to no sum to each). Large tiles / these: D = 512,

@@ -1,0 +1,38 @@
+"""Which tiles the token statistics and the 8-bit product take, from the library's own rules (host code, compiled here)."""
+import ctypes
+import os
+import shutil
+import subprocess
+
+import pytest
+
+from paper_2603_04135_amd import build as B
+
+FEW, T128x96, T128x128, T256x192, T256x256 = range(5)
+ROWS, COLUMNS = {T128x96: 128, T128x128: 128, T256x192: 256, T256x256: 256}, {T128x96: 96, T128x128: 128, T256x192: 192, T256x256: 256}
+SOURCE = """
+#include "stats_plan.h"
+extern "C" int tile(int n, int V, int k2, int i8) { return dppo::logits_tile(n, V, k2, i8 != 0); }
+extern "C" int eight(int n, int V, int k2) { return dppo::eight_wavefronts(n, V, k2); }
+"""
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    d = tmp_path_factory.mktemp("plan")
+    src, so = str(d / "plan.cpp"), str(d / "plan.so")
+    with open(src, "w") as f:
+        f.write(SOURCE)
+    subprocess.run([shutil.which("g++") or "c++", "-std=c++17", "-shared", "-fPIC", "-I", B.CSRC, src, "-o", so], check=True)
+    return ctypes.CDLL(so)
+
+
+def test_launches_stay_below_2_to_the_32_threads(plan):
+    """The runtime launches the number of threads modulo 2^32. Chunks have at most 2^31 logits, and 256 tokens in any case."""
+    for V in (2 ** 30, 2 ** 30 - 1, 2 ** 30 - 128, 2 ** 29, 2 ** 27 + 1, 2 ** 23, 2 ** 20 + 1, 151936, 1000):
+        for n in (17, 64, 96, 97, 100, 128, 129, 192, 193, 255, 256, max(256, min(32768, 2 ** 31 // V))):
+            for k2 in (64, 128, 512, 576, 4096):
+                for i8 in (0, 1):
+                    t = plan.tile(n, V, k2, i8)
+                    threads = 256 if t == T128x96 or t == T128x128 and not plan.eight(n, V, k2) else 512
+                    assert -(-V // ROWS[t]) * -(-n // COLUMNS[t]) * threads < 2 ** 32, (n, V, k2, t)
