@@ -28,6 +28,19 @@ int check_launch(const char* what) {
     return DPPO_OK;
 }
 
+// (Arguments are also checked on hosts without a device, where a status word is no address of one: that is left alone.)
+int finish_without_tokens(const char* what, int32_t* status, hipStream_t st) {
+    if (!status) return DPPO_OK;
+    hipPointerAttribute_t memory;
+    if (hipPointerGetAttributes(&memory, status) != hipSuccess) {
+        (void)hipGetLastError();
+        return DPPO_OK;
+    }
+    if (memory.type == hipMemoryTypeUnregistered) return DPPO_OK;
+    launch_fill_zero(nullptr, 0, status, st);
+    return check_launch(what);
+}
+
 namespace {
 
 // ---- optional stage timing (benchmarks): HIP events around the launches of each stage, on the
@@ -484,7 +497,7 @@ int dppo_token_logprob(const dppo_head_shape* shape, const void* H, const void* 
     int rc = validate_shape(shape);
     if (rc != DPPO_OK) return rc;
     const dppo_head_shape& s = *shape;
-    if (s.N == 0) return DPPO_OK;
+    if (s.N == 0) return finish_without_tokens("dppo_token_logprob", status, (hipStream_t)stream);
     if (!H || !W || !ids || !logp) return fail(DPPO_ERR_INVALID_ARG, "a required array pointer is NULL");
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255u)) return fail(DPPO_ERR_WORKSPACE, "workspace is NULL or not 256-byte aligned");
     if (s.dtype == 1 && (!aligned16(H) || !aligned16(W))) return fail(DPPO_ERR_INVALID_ARG, "H and W must be 16-byte aligned");
@@ -521,7 +534,7 @@ int dppo_token_logprob_noalloc(const dppo_head_shape* shape, const void* H, cons
                     "shape needs at least %zu bytes of scratch (one 256-token chunk of D=%d, V=%d), above the fixed %zu bytes "
                     "of dppo_token_logprob_noalloc; use dppo_token_logprob with a workspace",
                     q.total, shape->D, shape->V, STATIC_SCRATCH_BYTES);
-    if (shape->N == 0) return DPPO_OK;
+    if (shape->N == 0) return finish_without_tokens("dppo_token_logprob_noalloc", status, (hipStream_t)stream);
     void* ws = nullptr;
     if ((rc = static_scratch(&ws)) != DPPO_OK) return rc;
     return dppo_token_logprob(shape, H, W, ids, loss_pos, logp, lse, status, ws, STATIC_SCRATCH_BYTES, stream);

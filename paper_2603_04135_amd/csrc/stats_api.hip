@@ -165,7 +165,7 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k, const void* H,
     int rc = validate(shape, top_k, false);
     if (rc != DPPO_OK) return rc;
     const dppo_head_shape& s = *shape;
-    if (s.N == 0) return DPPO_OK;
+    if (s.N == 0) return finish_without_tokens("dppo_token_stats", status, (hipStream_t)stream);
     if (!H || !W) return fail(DPPO_ERR_INVALID_ARG, "H and W must not be NULL");
     if ((s.dtype == I8) != (h_scale != nullptr) || (s.dtype == I8) != (w_scale != nullptr))
         return fail(DPPO_ERR_INVALID_ARG, "h_scale and w_scale belong to int8 operands and to no others");

@@ -817,3 +817,26 @@ def test_quantize_more_rows_than_a_launch_has_threads_for(P):
     words = q.view(torch.int64)                  # (a row's first word holds its one value, the other fifteen nothing)
     assert torch.equal(words[:, 0] & 255, q[:, 0].to(torch.int64) & 255) and (words[:, 0] >> 8 == 0).all()
     assert words[:, 1:].count_nonzero() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "i8"])
+def test_status_of_a_call_without_loss_tokens(P, dtype):
+    """The status word is cleared where there is nothing to do, too: what an earlier call reported is gone."""
+    c = Case(dtype, 5, 128, 300, seed=41)
+    none, word = torch.zeros(0, dtype=torch.int32, device=DEV), torch.full((1,), 77, dtype=torch.int32, device=DEV)
+    at, c.loss_pos = c.loss_pos, none
+    for k in (0, 3):
+        out = c.call(P, k, status=word.fill_(77))
+        assert word.item() == 0 and out["lse"].shape == (0,)
+    if dtype == "i8":
+        return
+    z = torch.zeros(0, device=DEV)
+    P.dppo_token_stats_bwd(c.H, c.W, c.ids, none, z, z, g_logp=z, status=word.fill_(77))
+    assert word.item() == 0
+    P.dppo_token_logprob(c.H, c.W, c.ids, none, status=word.fill_(77))
+    assert word.item() == 0
+    P.dppo_token_logprob_noalloc(c.H, c.W, c.ids, none, z, status=word.fill_(77))
+    assert word.item() == 0
+    c.loss_pos = at                              # (and no error is left behind)
+    c.call(P, 3, status=word.fill_(77))
+    assert word.item() == 0
