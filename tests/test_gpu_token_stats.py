@@ -840,3 +840,44 @@ def test_status_of_a_call_without_loss_tokens(P, dtype):
     c.loss_pos = at                              # (and no error is left behind)
     c.call(P, 3, status=word.fill_(77))
     assert word.item() == 0
+
+
+# 8-bit operands by each of the wide tiles, neither tokens nor vocabulary a multiple of them (tests/test_stats_plan.py holds these to their tiles)
+I8_TILES = [("256x256", 1100, 128, 60001), ("256x256", 700, 384, 40001), ("256x192", 300, 128, 70001), ("256x192", 513, 256, 20011)]
+
+
+@pytest.mark.parametrize("tile,N,D,V", I8_TILES)
+@pytest.mark.parametrize("positions", ["loss_pos", "identity", "no targets"])
+@pytest.mark.parametrize("k", [0, 20])
+def test_statistics_of_8_bit_operands_by_wide_tiles(P, tile, N, D, V, positions, k):
+    c = Case("i8", N, D, V, seed=42, extra=None if positions == "loss_pos" else 0, targets=positions != "no targets")
+    check_stats(c.call(P, k), c.logits(), c.rows()[1], k)
+
+
+@pytest.mark.parametrize("tile,T,D,V", I8_TILES)
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_matmul_i8_by_wide_tiles(P, tile, T, D, V, out):
+    c = Case("i8", T, D, V, seed=43, extra=0)
+    room = torch.full((T * V + 64,), 7.0, dtype=out, device=DEV)
+    P.dppo_matmul_i8(c.H, c.h_scale, c.W, c.w_scale, out=room[:T * V].view(T, V))
+    want = (c.H.double() @ c.W.double().T).float() * c.w_scale * c.h_scale[:, None]
+    assert torch.equal(room[:T * V].view(T, V), want.to(out)) and (room[T * V:] == 7).all()
+
+
+# more than 4096 + D tokens and no small gradient: dH reads a transposed copy of W
+GRADIENT_BY_A_COPY = [(4200, 64, 4099), (4300, 128, 5003)]
+
+
+@pytest.mark.parametrize("N,D,V", GRADIENT_BY_A_COPY)
+@pytest.mark.parametrize("out", [torch.float32, torch.bfloat16])
+def test_gradient_by_a_transposed_copy_of_the_vocabulary(P, N, D, V, out):
+    """In one chunk, in a workspace full of NaN, and in chunks that share the copy."""
+    c = Case("bf16", N, D, V, seed=44)
+    g = make_grads(c, 9, ALL)
+    what = 2 if out == torch.bfloat16 else 1
+    most = P.dppo_token_stats_workspace_bytes(c.T, N, D, V, 1, 0, what)
+    least = P.dppo_token_stats_workspace_min_bytes(c.T, N, D, V, 1, 0, what)
+    assert least < most
+    for nbytes in (most, (least + most) // 2, least):
+        ws = P.binding.alloc_workspace(nbytes, DEV).fill_(0xFF)
+        check_grads(c, g, backward(P, c, g, ws=ws, dW_dtype=out))

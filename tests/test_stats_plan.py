@@ -7,6 +7,7 @@ import subprocess
 import pytest
 
 from paper_2603_04135_amd import build as B
+from test_gpu_token_stats import GRADIENT_BY_A_COPY, I8_TILES
 
 FEW, T128x96, T128x128, T256x192, T256x256 = range(5)
 ROWS, COLUMNS = {T128x96: 128, T128x128: 128, T256x192: 256, T256x256: 256}, {T128x96: 96, T128x128: 128, T256x192: 192, T256x256: 256}
@@ -14,6 +15,7 @@ SOURCE = """
 #include "stats_plan.h"
 extern "C" int tile(int n, int V, int k2, int i8) { return dppo::logits_tile(n, V, k2, i8 != 0); }
 extern "C" int eight(int n, int V, int k2) { return dppo::eight_wavefronts(n, V, k2); }
+extern "C" int small_grad(int N, int D, int V) { return dppo::small_grad(N, D, V); }
 """
 
 
@@ -36,3 +38,11 @@ def test_launches_stay_below_2_to_the_32_threads(plan):
                     t = plan.tile(n, V, k2, i8)
                     threads = 256 if t == T128x96 or t == T128x128 and not plan.eight(n, V, k2) else 512
                     assert -(-V // ROWS[t]) * -(-n // COLUMNS[t]) * threads < 2 ** 32, (n, V, k2, t)
+
+
+def test_gpu_tests_reach_the_tiles_they_are_meant_for(plan):
+    for name, n, D, V in I8_TILES:
+        assert plan.tile(n, V, D // 2, 1) == {"256x256": T256x256, "256x192": T256x192}[name]
+        assert n % COLUMNS[plan.tile(n, V, D // 2, 1)] and V % 256
+    for N, D, V in GRADIENT_BY_A_COPY:
+        assert N > 4096 + D and not plan.small_grad(N, D, V)
