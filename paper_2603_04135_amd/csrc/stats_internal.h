@@ -45,7 +45,6 @@ void launch_stats_rows(const float* Z, int64_t ldz, const TokenArgs& a, const St
 // Statistics of the vocabulary GEMM by groups of rows, STATS_GROUPS of a tile (a unit of the kernel for few tokens is one): mx[at(g, n)]
 // is group g's maximum for token n, sd[at(g, n)] = {sum, dev} against it; zy[n]: target logits (or NULL). A token's groups lie side by side
 // up to JOIN_ALONE tokens, which a workgroup each joins, beyond that the tokens of a group.
-constexpr int JOIN_ALONE = 256;
 struct StatsPart {
     float* mx; float2* sd; float* zy; int32_t group_step, token_step;
     __device__ __forceinline__ size_t at(int g, int n) const { return (size_t)g * group_step + (size_t)n * token_step; }

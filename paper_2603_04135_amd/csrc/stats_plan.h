@@ -49,6 +49,13 @@ inline bool eight_wavefronts(int32_t n, int32_t V, int32_t k2) {
     return tiles <= 256 || (k2 <= 512 && tiles < (int64_t)1 << 23);       // (2^23 tiles of 512 threads are more than a launch has)
 }
 
+// Tokens that a workgroup joins: the more, the more of them read the maxima side by side; the fewer, the more workgroups. us with 4 / 8 / 16, 20
+// alternatives: V = 151936, 400 tokens 21.3 / 22.1 / 26.5, 512 22.7 / 22.3 / 26.4, 1000 27.2 / 23.6 / 27.4, 2048 57 / 30.1 / 28.8, 2500 72 / 53 / 34,
+// 8000 208 / 122 / 86; V = 32000, 512 15.5 / 15.9 / 18.3, 700 16.2 / 16.3 / 18.4, 1000 17.2 / 16.5 / 18.3, 2048 33 / 19.2 / 19.0; none: V = 151936, 400
+// 6.7 / 6.4 / 7.2, 1000 12.5 / 8.0 / 8.2.
+constexpr int JOIN_ALONE = 256;                   // (a token's groups lie side by side up to here, see StatsPart)
+inline int join_tokens(int32_t n) { return n <= JOIN_ALONE ? 1 : n <= 512 ? 4 : n <= 2048 ? 8 : 16; }
+
 // Whether the gradient goes by tiles of 128 x 128 (see SmallGrad): problems that large ones leave much of the chip idle in. One chunk, no more than a
 // chip of large tiles of entries, and of dW few (or next to no sum to each). Large tiles / these: D = 512,
 // V = 5000: 60 tokens 44 / 30 us, 1000 80 / 58; D = 2560, V = 3000: 60 68 / 52, 2500 193 / 149; D = 256, V = 20000: 300 68 / 52; D = 1024, V =

@@ -516,12 +516,12 @@ void launch_stats_join(const StatsPart& part, int rows, const float* Z, int64_t 
         if (o.top_k > 0) stats_join_kernel<TOK, true><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
         else stats_join_kernel<TOK, false><<<blocks, JOIN_THREADS, 0, st>>>(part, rows, Z, ldz, a, look_up, o, cv);
     };
-    // As many tokens a workgroup as leave every compute unit at most one. V = 151936, 20 alternatives, 4 / 8 / 16 tokens: 1000 tokens 27.5 /
-    // 24.2 / 30.3 us, 2000 55 / 31 / 32, 8000 211 / 123 / 90.
-    if (cv.n_c <= JOIN_ALONE) go(std::integral_constant<int, 1>{});
-    else if (cv.n_c <= 4 * DEFAULT_CUS) go(std::integral_constant<int, 4>{});
-    else if (cv.n_c <= 8 * DEFAULT_CUS) go(std::integral_constant<int, 8>{});
-    else go(std::integral_constant<int, 16>{});
+    switch (join_tokens(cv.n_c)) {
+        case 1: go(std::integral_constant<int, 1>{}); break;
+        case 4: go(std::integral_constant<int, 4>{}); break;
+        case 8: go(std::integral_constant<int, 8>{}); break;
+        default: go(std::integral_constant<int, 16>{});
+    }
 }
 
 void launch_stats_bound(const StatsPart& part, int32_t groups, int32_t top_k, ChunkView cv, float* tau, hipStream_t st) {

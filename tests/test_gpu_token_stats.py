@@ -881,3 +881,11 @@ def test_gradient_by_a_transposed_copy_of_the_vocabulary(P, N, D, V, out):
     for nbytes in (most, (least + most) // 2, least):
         ws = P.binding.alloc_workspace(nbytes, DEV).fill_(0xFF)
         check_grads(c, g, backward(P, c, g, ws=ws, dW_dtype=out))
+
+
+@pytest.mark.parametrize("N", [256, 257, 512, 513, 2048, 2049])
+@pytest.mark.parametrize("dtype,k", [("bf16", 20), ("bf16", 0), ("i8", 3)])
+def test_statistics_on_both_sides_of_the_joins(P, N, dtype, k):
+    """1, 4, 8 and 16 tokens a workgroup of the join."""
+    c = Case(dtype, N, 128, 9001, seed=45)
+    check_stats(c.call(P, k), c.logits(), c.rows()[1], k)

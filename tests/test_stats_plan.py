@@ -15,6 +15,7 @@ SOURCE = """
 #include "stats_plan.h"
 extern "C" int tile(int n, int V, int k2, int i8) { return dppo::logits_tile(n, V, k2, i8 != 0); }
 extern "C" int eight(int n, int V, int k2) { return dppo::eight_wavefronts(n, V, k2); }
+extern "C" int join_tokens(int n) { return dppo::join_tokens(n); }
 extern "C" int small_grad(int N, int D, int V) { return dppo::small_grad(N, D, V); }
 """
 
@@ -46,3 +47,9 @@ def test_gpu_tests_reach_the_tiles_they_are_meant_for(plan):
         assert n % COLUMNS[plan.tile(n, V, D // 2, 1)] and V % 256
     for N, D, V in GRADIENT_BY_A_COPY:
         assert N > 4096 + D and not plan.small_grad(N, D, V)
+
+
+def test_tokens_of_a_join(plan):
+    """Both sides of each line (see join_tokens for what was measured there)."""
+    for n, tokens in ((1, 1), (256, 1), (257, 4), (512, 4), (513, 8), (1000, 8), (2048, 8), (2049, 16), (8191, 16)):
+        assert plan.join_tokens(n) == tokens
