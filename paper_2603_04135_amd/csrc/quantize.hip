@@ -136,7 +136,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const E* __restrict_
     }
 }
 
-constexpr int64_t FEW_ROWS = 2048;
+constexpr int64_t FEW_ROWS = 2048, MANY_ROWS = 16384;
 template <class E>
 void launch(const E* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float* scale, hipStream_t st) {
     auto go = [&](auto nv, auto wpr) {
@@ -151,9 +151,13 @@ void launch(const E* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float
     };
     const std::integral_constant<int, 1> one;
     const std::integral_constant<int, 4> four;
-    // a workgroup per row where there are few or they are long: their loads and divisions in a quarter of the time. One row of D = 4096
-    // 5.0 -> 2.5 us, 1024 7.8 -> 5.3, 4096 14.5 -> 12.1, but of D = 1000 5.1 -> 7.3.
-    if ((rows <= FEW_ROWS && pitch > 512) || pitch > 4096) {
+    // A workgroup per row, its loads and divisions in a quarter of the time, where rows are long or few. us, a wavefront / a workgroup per row,
+    // bfloat16: D = 4096, 1024 rows 6.8 / 4.9, 4096 14.0 / 11.8, 151936 332 / 314; 3200, 151936 282 / 275; 2560, 1024 5.0 / 4.0, 8192 16.3 / 14.6,
+    // 32768 42.9 / 44.1, 151936 215 / 243; 2048, 2048 5.5 / 5.1, 4096 7.4 / 8.0; 1024, 2048 4.0 / 4.0, 4096 4.9 / 6.0. Many long rows
+    // of bfloat16 that begin off 16-byte addresses stay with a wavefront each: 3001, 8192 19.7 / 17.3, 16384 31.0 / 29.6, 32768 66 / 71, 151936 277 / 314;
+    // 4095, 16384 45 / 43, 151936 453 / 481. float32: 4096, 4096 15.6 / 13.5, 151936 547 / 538; 4095, 151936 582 / 539; 2048, 2048 5.2 / 5.2, 4096 7.6 / 8.7.
+    const bool many = sizeof(E) == 2 && D % 8 != 0 && rows > MANY_ROWS;
+    if ((rows <= FEW_ROWS && pitch > 512) || (pitch > 2560 && !many) || pitch > 4096) {
         if (pitch <= 2048) go(std::integral_constant<int, 1>{}, four);
         else if (pitch <= 4096) go(std::integral_constant<int, 2>{}, four);
         else if (pitch <= 8192) go(std::integral_constant<int, 4>{}, four);
@@ -162,7 +166,7 @@ void launch(const E* X, int64_t rows, int32_t D, int8_t* q, int64_t pitch, float
     } else if (pitch <= 512) go(std::integral_constant<int, 1>{}, one);
     else if (pitch <= 1024) go(std::integral_constant<int, 2>{}, one);
     else if (pitch <= 2048) go(std::integral_constant<int, 4>{}, one);
-    else if (pitch <= 2560) go(std::integral_constant<int, 5>{}, one);
+    else if (pitch <= 2560) go(std::integral_constant<int, 5>{}, one);     // (with registers for 4096 elements 151936 rows of 2176 take 207 us, not 174)
     else go(std::integral_constant<int, 8>{}, one);
 }
 

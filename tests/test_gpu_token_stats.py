@@ -889,3 +889,17 @@ def test_statistics_on_both_sides_of_the_joins(P, N, dtype, k):
     """1, 4, 8 and 16 tokens a workgroup of the join."""
     c = Case(dtype, N, 128, 9001, seed=45)
     check_stats(c.call(P, k), c.logits(), c.rows()[1], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows", [2048, 2049, 16384, 16385])
+@pytest.mark.parametrize("D", [500, 640, 2047, 2553, 2568, 3001, 4096, 4097])
+def test_quantize_rows_on_both_sides_of_every_rule(P, dtype, rows, D):
+    """A wavefront or a workgroup per row, with registers for 512 to 4096 elements, at lengths that are multiples of 8 and not."""
+    gen = torch.Generator(device=DEV).manual_seed(rows + D)
+    x = (torch.randn((rows, D), generator=gen, device=DEV) * torch.exp(torch.randn((rows, 1), generator=gen, device=DEV) * 3)).to(DTYPES[dtype])
+    q, scale = P.dppo_quantize_rows(x)
+    top = x.float().abs().amax(dim=1)
+    assert torch.equal(scale, top * torch.tensor(1 / 127, dtype=torch.float32, device=DEV))
+    want = (x.double() / scale.double()[:, None]).float().round()        # (a quotient that 64 bits round to 32 is the 32-bit quotient)
+    assert torch.equal(q[:, :D], want.to(torch.int8)) and (q[:, D:] == 0).all()
