@@ -319,7 +319,8 @@ int dppo_token_stats(const dppo_head_shape* shape, int32_t top_k,
  *   dH[T,D] = dz W (dtype of H; rows that are no loss rows are zero),  dW[V,D] = dz^T H.
  * dW_dtype 0: float32, added to the buffer's contents if accumulate_dW != 0. dW_dtype 1: bfloat16 (bfloat16 operands only),
  * overwritten: the float32 sum over all tokens, rounded once. dW is used for partial sums of dH before it is written.
- * bfloat16 operands: dz is rounded to bfloat16 as an operand of the two products. dtype 2 has no gradient. A token whose lse or
+ * bfloat16 operands: dz is formed in float32 and rounded to bfloat16 as an operand of the two products, for either type of dW (an error of some 1.7e-3 of
+ * the norm of dW and dH, as much as the rounding of a bfloat16 result); their sums are float32. dtype 2 has no gradient. A token whose lse or
  * entropy is not finite (see above) has a NaN dz, which reaches all of dW: leave it out of loss_pos. Entries of loss_pos must be
  * distinct here (not checked); dppo_token_stats takes them in any order and more than once. */
 typedef struct {

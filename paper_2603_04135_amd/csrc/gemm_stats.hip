@@ -21,6 +21,7 @@ constexpr int GRAD_FEW_TILES = 128;
 // four / eight). Deeper rings of slices are no faster: two workgroups no longer fit a compute unit.
 typedef Cfg128Eight CfgSmall;
 static_assert(CfgSmall::BN == SMALL_BLOCK_ROWS && CfgSmall::BK == GEMM_B_BLOCK_K, "the blocks of HT");
+static_assert((size_t)SMALL_PARTS_MOST * CfgSmall::BM * CfgSmall::BN <= (size_t)256 * CfgBig::BM * CfgBig::BN, "partial tiles fit mfma_dw_partial_bytes()");
 
 hipError_t allow_all() {
     hipError_t e = allow_logits<EpiStats<false, false>>();

@@ -342,8 +342,6 @@ __global__ __launch_bounds__(1024) void stats_bound_kernel(StatsPart part, int32
     if (lane == 0 && my_n < n_c) tau[my_n] = top_value(lane_value(top.entry, top_k - 1));
 }
 
-// A wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row (16-byte vectors, zero beyond
-// n_c) and its scale. Bound by HBM.
 // Row of H of chunk token n, clamped (what is wrong with it is reported elsewhere).
 __device__ __forceinline__ int64_t token_row(const TokenArgs& a, ChunkView cv, int n) {
     const int64_t row = a.loss_pos ? (int64_t)a.loss_pos[cv.n0 + n] : cv.n0 + n;
@@ -378,7 +376,8 @@ __device__ void transpose_tokens(const GatherRows& g, ChunkView cv, int block, u
         *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.transpose) + off) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
-// Workgroup `block` of `blocks`.
+// Workgroup `block` of `blocks`. The first gather, a wavefront per row of the chunk: target and (clamped) row of H of the token, a copy of the row
+// (16-byte vectors, zero beyond n_c) and its scale, bound by HBM; the next transpose; the last clear.
 struct GatherBlocks { unsigned gather, transpose, all; };
 __device__ __forceinline__ void gather_rows(const GatherRows& g, ChunkView cv, unsigned block, const GatherBlocks& blocks, uint16_t (*tile)[64 + 2]) {
     if (block >= blocks.gather + blocks.transpose) {
