@@ -884,22 +884,149 @@ def test_gradient_by_a_transposed_copy_of_the_vocabulary(P, N, D, V, out):
 
 
 @pytest.mark.parametrize("N", [256, 257, 512, 513, 2048, 2049])
-@pytest.mark.parametrize("dtype,k", [("bf16", 20), ("bf16", 0), ("i8", 3)])
-def test_statistics_on_both_sides_of_the_joins(P, N, dtype, k):
+def test_statistics_on_both_sides_of_the_joins(P, N):
     """1, 4, 8 and 16 tokens a workgroup of the join."""
-    c = Case(dtype, N, 128, 9001, seed=45)
-    check_stats(c.call(P, k), c.logits(), c.rows()[1], k)
+    for dtype, k in (("bf16", 20), ("bf16", 0), ("i8", 3)):
+        c = Case(dtype, N, 128, 9001, seed=45)
+        check_stats(c.call(P, k), c.logits(), c.rows()[1], k)
+
+
+@pytest.mark.parametrize("D", [500, 640, 2047, 2553, 2568, 3001, 4096, 4097])
+def test_quantize_rows_on_both_sides_of_every_rule(P, D):
+    """A wavefront or a workgroup per row, with registers for 512 to 4096 elements, at lengths that are multiples of 8 and not."""
+    gen = torch.Generator(device=DEV).manual_seed(D)
+    most = torch.randn((16385, D), generator=gen, device=DEV) * torch.exp(torch.randn((16385, 1), generator=gen, device=DEV) * 3)
+    for dtype in DTYPES.values():
+        for rows in (2048, 2049, 16384, 16385):
+            x = most[:rows].to(dtype)
+            q, scale = P.dppo_quantize_rows(x)
+            top = x.float().abs().amax(dim=1)
+            assert torch.equal(scale, top * torch.tensor(1 / 127, dtype=torch.float32, device=DEV))
+            want = (x.double() / scale.double()[:, None]).float().round()    # (a quotient that 64 bits round to 32 is the 32-bit quotient)
+            assert torch.equal(q[:, :D], want.to(torch.int8)) and (q[:, D:] == 0).all()
+
+
+def raw_stats(P, c, k, outputs, status=None, chunk_bytes=None):
+    """dppo_token_stats through the C entry, with only the given outputs (the others NULL)."""
+    import ctypes
+    B = P.binding
+    shape = B.HeadShape(c.T, c.N, c.D, c.V, {"f32": 0, "bf16": 1, "i8": 2}[c.dtype])
+    ws = B.alloc_workspace(chunk_bytes or P.dppo_token_stats_workspace_bytes(c.T, c.N, c.D, c.V, shape.dtype, k), DEV).fill_(0xFF)
+    f32 = dict(dtype=torch.float32, device=DEV)
+    out = {n: torch.full((c.N,), float("nan"), **f32) for n in outputs}
+    if k:
+        out["top_ids"] = torch.full((c.N, k), -1, dtype=torch.int32, device=DEV)
+        out["top_logp"] = torch.full((c.N, k), float("nan"), **f32)
+    ptr = lambda t: None if t is None else t.data_ptr()
+    lib = P.load()
+    assert lib.dppo_token_stats(ctypes.byref(shape), k, ptr(c.H), ptr(c.W), ptr(c.h_scale), ptr(c.w_scale), ptr(c.ids), ptr(c.loss_pos),
+                                *[ptr(out.get(n)) for n in ("logp", "lse", "entropy", "top_ids", "top_logp")], ptr(status), ptr(ws),
+                                ws.numel(), torch.cuda.current_stream().cuda_stream) == 0, lib.dppo_last_error()
+    return out
+
+
+@pytest.mark.parametrize("dtype,N,V", [("f32", 3, 20011), ("f32", 90, 600), ("bf16", 3, 9001), ("bf16", 90, 9001), ("bf16", 300, 9001),
+                                       ("bf16", 1100, 60001), ("i8", 3, 9001), ("i8", 1100, 60001)])
+def test_each_output_by_itself(P, dtype, N, V):
+    """What is not asked for may be NULL, in any combination, and changes nothing else."""
+    c = Case(dtype, N, 128, V, seed=50)
+    want = c.call(P, 5)
+    for k, outputs in ((0, ["logp"]), (0, ["lse"]), (0, ["entropy"]), (5, []), (5, ["entropy"]), (0, ["logp", "entropy"])):
+        out = raw_stats(P, c, k, outputs)
+        assert set(out) == set(outputs) | ({"top_ids", "top_logp"} if k else set())
+        for n in out:
+            assert torch.equal(out[n], want[n]), (n, k, outputs)
+
+
+@pytest.mark.parametrize("dtype,N,D,V,k", [("f32", 40001, 16, 300, 3), ("bf16", 40001, 64, 300, 3), ("i8", 40001, 128, 300, 0), ("bf16", 3000, 128, 5003, 20),
+                                           ("f32", 3000, 33, 1003, 20), ("i8", 3000, 128, 5003, 20)])
+@pytest.mark.parametrize("positions", ["loss_pos", "identity"])
+def test_statistics_in_chunks_of_any_size(P, dtype, N, D, V, k, positions):
+    """More tokens than one chunk holds, and workspaces between the smallest and the recommended one."""
+    c = Case(dtype, N, D, V, seed=51, extra=None if positions == "loss_pos" else 0)
+    code = {"f32": 0, "bf16": 1, "i8": 2}[dtype]
+    least, most = (f(c.T, N, D, V, code, k) for f in (P.dppo_token_stats_workspace_min_bytes, P.dppo_token_stats_workspace_bytes))
+    z, y = c.logits(), c.rows()[1]
+    for part in (0.0, 0.3, 0.77, 1.0):
+        ws = P.binding.alloc_workspace(least + int((most - least) * part), DEV).fill_(0xFF)
+        check_stats(c.call(P, k, ws=ws), z, y, k)
+
+
+@pytest.mark.parametrize("dtype,N,D,V", [("f32", 40001, 8, 100), ("bf16", 40001, 64, 100), ("bf16", 9000, 128, 3001)])
+@pytest.mark.parametrize("positions", ["loss_pos", "identity"])
+def test_gradient_of_more_than_a_chunk(P, dtype, N, D, V, positions):
+    c = Case(dtype, N, D, V, seed=52, extra=None if positions == "loss_pos" else 0)
+    g = make_grads(c, 53, ALL)
+    check_grads(c, g, backward(P, c, g))
+    dW0 = torch.randn(c.W.shape, device=DEV)
+    check_grads(c, g, backward(P, c, g, dW=dW0.clone(), accumulate_dW=True), dW0)
+    if dtype == "bf16":
+        check_grads(c, g, backward(P, c, g, dW_dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("N", [0, 5, 300])
+def test_float32_operands_at_any_address(P, N):
+    """float32 needs no more than 4-byte alignment, of any matrix."""
+    c = Case("f32", max(N, 1), 64, 513, seed=54)
+    if N == 0:
+        c.N, c.loss_pos = 0, c.loss_pos[:0]
+
+    def moved(t, fill=None):
+        room = torch.full((t.numel() + 8,), 7.0, device=DEV)
+        m = room[1:1 + t.numel()].view(t.shape)
+        m.copy_(t) if fill is None else m.fill_(fill)
+        return room, m
+
+    want = c.call(P, 5)
+    g = make_grads(c, 1, ALL) if N else dict(g_logp=torch.zeros(0, device=DEV))
+    ref = P.dppo_token_stats_bwd(c.H, c.W, c.ids, c.loss_pos, want["lse"], want["entropy"], **g)
+    H, W = c.H, c.W
+    (_, c.H), (_, c.W) = moved(H), moved(W)
+    got = c.call(P, 5)
+    for n in want:
+        assert torch.equal(got[n], want[n]), n
+    (room_h, dH), (room_w, dW) = moved(H, float("nan")), moved(W, float("nan"))
+    P.dppo_token_stats_bwd(c.H, c.W, c.ids, c.loss_pos, want["lse"], want["entropy"], dH=dH, dW=dW, **g)
+    assert torch.equal(dH, ref["dH"]) and torch.equal(dW, ref["dW"])
+    for room in (room_h, room_w):
+        assert room[0] == 7 and (room[-7:] == 7).all()
+    if N == 0:
+        dW.fill_(3.0)
+        P.dppo_token_stats_bwd(c.H, c.W, c.ids, c.loss_pos, want["lse"], want["entropy"], dH=dH, dW=dW, accumulate_dW=True, **g)
+        assert (dW == 3).all() and (dH == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("rows", [2048, 2049, 16384, 16385])
-@pytest.mark.parametrize("D", [500, 640, 2047, 2553, 2568, 3001, 4096, 4097])
-def test_quantize_rows_on_both_sides_of_every_rule(P, dtype, rows, D):
-    """A wavefront or a workgroup per row, with registers for 512 to 4096 elements, at lengths that are multiples of 8 and not."""
-    gen = torch.Generator(device=DEV).manual_seed(rows + D)
-    x = (torch.randn((rows, D), generator=gen, device=DEV) * torch.exp(torch.randn((rows, 1), generator=gen, device=DEV) * 3)).to(DTYPES[dtype])
+@pytest.mark.parametrize("rows,D", [(5, 640), (3000, 333), (3, 5000)])
+def test_quantize_rows_at_any_address(P, dtype, rows, D):
+    gen = torch.Generator(device=DEV).manual_seed(55)
+    room = torch.randn(rows * D + 9, generator=gen, device=DEV).to(DTYPES[dtype])
+    x = room[1:1 + rows * D].view(rows, D)
     q, scale = P.dppo_quantize_rows(x)
-    top = x.float().abs().amax(dim=1)
-    assert torch.equal(scale, top * torch.tensor(1 / 127, dtype=torch.float32, device=DEV))
-    want = (x.double() / scale.double()[:, None]).float().round()        # (a quotient that 64 bits round to 32 is the 32-bit quotient)
-    assert torch.equal(q[:, :D], want.to(torch.int8)) and (q[:, D:] == 0).all()
+    q0, scale0 = P.dppo_quantize_rows(x.clone())
+    assert torch.equal(q, q0) and torch.equal(scale, scale0)
+
+
+@pytest.mark.parametrize("dtype,N,V", [("bf16", 3, 9001), ("i8", 16, 9001), ("bf16", 1100, 60001), ("i8", 1100, 60001), ("f32", 2, 20011)])
+def test_every_kernel_of_the_statistics_captured(P, dtype, N, V):
+    """Few tokens, and leading tiles with their bound, replayed with other inputs."""
+    c = Case(dtype, N, 128, V, seed=56)
+    ws = P.binding.alloc_workspace(P.dppo_token_stats_workspace_bytes(c.T, N, 128, V, {"f32": 0, "bf16": 1, "i8": 2}[dtype], 20), DEV)
+    c.call(P, 20, ws=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = c.call(P, 20, ws=ws)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    for _ in range(3):
+        if dtype == "i8":
+            c.H.copy_(torch.randint(-127, 128, c.H.shape, generator=gen, device=DEV, dtype=torch.int8))
+        else:
+            c.H.copy_(grid(c.H.shape, 1.0, 2.0 ** -4, gen, c.H.dtype))
+        want = {n: t.clone() for n, t in c.call(P, 20).items()}
+        ws.fill_(0xFF)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in want:
+            assert torch.equal(captured[n], want[n]), n
