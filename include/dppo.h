@@ -297,7 +297,8 @@ int dppo_loss_fwd_bwd(const dppo_head_shape* shape, const dppo_loss_params* p, i
  * Sums are float32 (against the maximum, so that neither lse nor entropy loses digits to large logits); logits at
  * -infinity carry no weight (a row of nothing else: lse -infinity, entropy and logp NaN). A row with a NaN logit or one at
  * +infinity has NaN results. top_ids are distinct and in [0, V) for every row. V is at most 2^30. ws must be 256-byte aligned; a smaller workspace than recommended means
- * smaller token chunks and does not change what a token's results are, except for their last bits.
+ * smaller token chunks and does not change what a token's results are, except for their last bits. Where top_k > 0, and for float32, the recommended one
+ * has room for all logits of a chunk in float32 (about 4 N V bytes, up to 8 GiB).
  */
 #define DPPO_TOP_K_MAX 64
 
@@ -338,8 +339,8 @@ int dppo_token_stats_bwd(const dppo_head_shape* shape, const dppo_stats_grad_par
 /* dppo_quantize_rows -- X[rows, D] (dtype 0 float32, 1 bfloat16, contiguous) to 8 bits with one scale per row, tokens and
  * vocabulary rows alike: scale[r] = max|X[r]| * (1/127), the reciprocal in float32, q[r, d] = X[r, d] / scale[r] (a correctly
  * rounded float32 division) rounded to the nearest integer, ties to even, in [-127, 127]. A zero row has scale 0 and q 0; a row
- * that holds an infinity or NaN has scale NaN and q 0. q has a row pitch of q_pitch bytes, a multiple of 128 of at least D; the
- * columns behind D are set to 0. */
+ * that holds an infinity or NaN has scale NaN and q 0. q is 16-byte aligned and has a row pitch of q_pitch bytes, a multiple of 128
+ * of at least D and at most 130944 (what the products take); the columns behind D are set to 0. X has the alignment of its elements. */
 int dppo_quantize_rows(int64_t rows, int32_t D, int32_t dtype, const void* X,
                        int8_t* q, int64_t q_pitch, float* scale, void* stream);
 

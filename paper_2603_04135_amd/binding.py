@@ -480,7 +480,8 @@ def dppo_token_stats(H, W, ids=None, loss_pos=None, top_k: int = 0, h_scale=None
                      ws: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None) -> dict:
     """H [T,D], W [V,D] float32, bfloat16, or int8 with h_scale [T] and w_scale [V] (dppo_quantize_rows); ids [T] int32
     or None (no logp). Returns dict(logp[N] or None, lse[N], entropy[N], top_ids[N,top_k] and top_logp[N,top_k], None for
-    top_k = 0) of device tensors; status: see dppo_token_logprob."""
+    top_k = 0) of device tensors; status: see dppo_token_logprob. The results share one allocation: one that is kept keeps the memory of
+    all, 3 + 2 top_k words a token; clone() what is to outlive the others."""
     lib = _lib or load()
     guard = _elsewhere(H)
     if guard is not None:

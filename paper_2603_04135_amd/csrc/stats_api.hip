@@ -11,7 +11,7 @@ enum { F32 = 0, BF16 = 1, I8 = 2 };
 constexpr int32_t I8_ROW = 128;             // 8-bit rows are whole GEMM slices
 constexpr int32_t I8_D_MAX = 130944;        // 128 * 128 * D stays below 2^31 (-128 is no result of quantisation, but a value)
 constexpr int32_t V_MAX = 1 << 30;
-// Stored logits of a forward chunk.
+// Logits of a forward chunk, where they are stored (elsewhere a bound alike: larger chunks gain nothing there).
 constexpr size_t LOGITS_CHUNK_BYTES = (size_t)8 << 30;
 
 struct Regions {                            // offsets into the workspace
