@@ -1030,3 +1030,18 @@ def test_every_kernel_of_the_statistics_captured(P, dtype, N, V):
         torch.cuda.synchronize()
         for n in want:
             assert torch.equal(captured[n], want[n]), n
+
+
+def test_no_loss_tokens_captured(P):
+    """All that such a call does is to clear its status word, on replays too."""
+    c = Case("bf16", 5, 64, 300, seed=57)
+    c.loss_pos = c.loss_pos[:0]
+    word, ws = torch.zeros(1, dtype=torch.int32, device=DEV), P.binding.alloc_workspace(1 << 20, DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.call(P, 3, ws=ws, status=word)
+    for _ in range(3):
+        word.fill_(77)
+        torch.cuda.synchronize()
+        graph.replay()
+        assert word.item() == 0
