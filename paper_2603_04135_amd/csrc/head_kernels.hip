@@ -753,7 +753,12 @@ void launch_seq_ratio(const int32_t* loss_cu, int32_t S, const float* logp, cons
 
 void launch_token_norm_coef(int32_t Q, int32_t G, const int32_t* comp_len, const float* coef, float* coef_out,
                             hipStream_t st) {
-    token_norm_coef_kernel<<<(unsigned)ceil_div(Q, 4), 256, 0, st>>>(Q, G, comp_len, coef, coef_out);
+    constexpr int64_t MOST = 1 << 25;            // (below 2^32 threads a launch: more run their number modulo 2^32, without an error)
+    for (int64_t q0 = 0; q0 < Q; q0 += MOST) {
+        const int32_t part = (int32_t)(Q - q0 < MOST ? Q - q0 : MOST);
+        const size_t at = (size_t)q0 * G;
+        token_norm_coef_kernel<<<(unsigned)ceil_div(part, 4), 256, 0, st>>>(part, G, comp_len + at, coef + at, coef_out + at);
+    }
 }
 
 void launch_grad_logits_f32(float* ZG, int32_t V, int32_t Vp, const int32_t* y, const float* lse, const float* c,

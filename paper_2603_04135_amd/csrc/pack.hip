@@ -511,8 +511,11 @@ void launch_pack(const dppo_pack_params& p, const int32_t* prompt_len, const int
 }
 
 void launch_gather_f32(int64_t n, const int32_t* idx, const float* src, float* dst, hipStream_t st) {
-    if (n <= 0) return;
-    gather_f32_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, st>>>(n, idx, src, dst);
+    constexpr int64_t MOST = (int64_t)1 << 31;   // (a launch of 2^32 threads or more runs what is left of their number in 32 bits, and reports nothing)
+    for (int64_t i0 = 0; i0 < n; i0 += MOST) {
+        const int64_t part = n - i0 < MOST ? n - i0 : MOST;
+        gather_f32_kernel<<<(unsigned)ceil_div(part, 256), 256, 0, st>>>(part, idx + i0, src, dst + i0);
+    }
 }
 
 }  // namespace dppo

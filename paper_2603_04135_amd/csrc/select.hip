@@ -322,8 +322,8 @@ __global__ void history_update_kernel(int n, const int32_t* __restrict__ prompt_
                                       const uint8_t* __restrict__ keep_prompt,
                                       const float* __restrict__ mean_abs_adv, float* __restrict__ hist_table,
                                       int64_t table_size) {
-    int b = blockIdx.x * blockDim.x + threadIdx.x;
-    if (b >= n) return;
+    const unsigned b = blockIdx.x * blockDim.x + threadIdx.x;      // (of n near 2^31 the last workgroup passes 31 bits)
+    if (b >= (unsigned)n) return;
     const int64_t q = prompt_index[b];
     if (keep_prompt[b] != 0 && q >= 0 && q < table_size) hist_table[q] = mean_abs_adv[b];
 }
@@ -408,7 +408,7 @@ void launch_select(const dppo_select_params& p, int n_bottom, const float* rewar
 void launch_history_update(int32_t n, const int32_t* prompt_index, const uint8_t* keep_prompt,
                            const float* mean_abs_adv, float* hist_table, int64_t table_size, hipStream_t st) {
     if (n <= 0) return;
-    history_update_kernel<<<(n + 255) / 256, 256, 0, st>>>(n, prompt_index, keep_prompt, mean_abs_adv, hist_table,
+    history_update_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, st>>>(n, prompt_index, keep_prompt, mean_abs_adv, hist_table,
                                                           table_size);
 }
 
