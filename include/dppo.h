@@ -394,8 +394,8 @@ int dppo_timing_read(double* ms /* [DPPO_N_STAGES] */, int64_t* launches /* [DPP
 /* Benchmark aid: where the workgroups of the three big GEMMs spend their time. counters: device array of
  * 12 uint64 the caller has zeroed, {vocabulary GEMM, dH GEMM, dW GEMM} x {shader cycles from the start of a
  * workgroup until its first operand slice is in LDS, cycles in the main loop, cycles in the epilogue, number of
- * workgroups}; while set, every whole-tile launch of the bfloat16 LM-head calls adds to it (4 atomic
- * adds per workgroup; the launches that split K are left out). NULL switches it off. Process-wide state,
+ * workgroups}; while set, every launch of 256 x 256 tiles by the bfloat16 and int8 LM-head calls adds to it (4 atomic
+ * adds per workgroup; the launches that split K and those of dppo_token_stats_bwd's gradient entries are left out). NULL switches it off. Process-wide state,
  * like the stage timing; the array must outlive the launches that write it. */
 int dppo_timing_tile_phases(uint64_t* counters);
 
